@@ -113,10 +113,11 @@ def _codes(x, block):
     g = x.view(gr, block, gc, 128)
     # in 64 bits, then rounded once: 32 lose what decides between two codes
     scale = (g.abs().amax(dim=(1, 3)).double() / E4M3_MAX).clamp_min(2.0 ** -126).float()
-    # the quotients rounded to 4 significant bits
+    # the quotients rounded to 4 significant bits (powers of two from their bits)
     v = g.double() / scale[:, None, :, None]
-    shift = 4 - torch.frexp(v).exponent.clamp_min(-5)
-    q = torch.ldexp(torch.round(torch.ldexp(v, shift)), -shift).float().to(torch.float8_e4m3fn)
+    shift = 4 - torch.frexp(v).exponent.clamp_min(-5).long()
+    up, down = (((shift * f + 1023) << 52).view(torch.float64) for f in (1, -1))
+    q = (torch.round(v * up) * down).float().to(torch.float8_e4m3fn)
     return q.view(gr * block, gc * 128)[:rows, :cols].contiguous(), scale
 
 
@@ -271,12 +272,13 @@ def work(case):
 # the definitions in 64 bits
 
 def _e4m3(v):
-    """v (float64) rounded to the nearest e4m3 value, ties to even; 2^-9 is the smallest step."""
-    a = v.abs()
-    e = torch.floor(torch.log2(a.clamp_min(2.0 ** -6)))
-    e = torch.where(torch.exp2(e) > a.clamp_min(2.0 ** -6), e - 1, e)
-    step = torch.exp2(e - 3)
-    return torch.sign(v) * torch.round(a / step).mul(step).clamp_max(E4M3_MAX)
+    """v (float64) rounded to the nearest e4m3 value, ties to the even code, by search."""
+    values = torch.arange(127, dtype=torch.uint8, device=v.device).view(torch.float8_e4m3fn).double()
+    borders = (values[1:] + values[:-1]) / 2
+    a = v.abs().contiguous()
+    code = torch.searchsorted(borders, a)
+    code += ((code < 126) & (a == borders[code.clamp_max(125)]) & (code % 2 == 1)).long()
+    return torch.sign(v) * values[code.clamp_max(126)]
 
 
 def _exact_quantize(st):
