@@ -79,7 +79,7 @@ enum {
                                 walk did not meet in time (a device fault; outputs undefined) */
 };
 
-/* element type of hidden states and LM-head weights (bias is always fp32) */
+/* element type of hidden states, LM-head weights and logits (bias is always fp32) */
 enum { DCD_F32 = 0, DCD_BF16 = 1 };
 
 /* row_stats slots (8 floats per row) */
@@ -287,12 +287,105 @@ int dcd_verify_greedy_noalloc(const dcd_problem *p, const dcd_inputs *in, const 
 /* bytes of device memory the allocation-free entry point holds per GPU */
 size_t dcd_noalloc_max_bytes(void);
 
+/* ------------------------------------------------------------------------
+ * The 8-bit proposal path: what a proposer does between a drafter's hidden states and
+ * dcd_verify_sample.  dcd_quantize_fp8 makes 8-bit codes of the hidden states of a step
+ * (and, once, of a head's weights), dcd_logits_fp8 multiplies them, dcd_sample draws a
+ * token per row and gives the probabilities it was drawn from, which are the draft_probs
+ * of a later dcd_verify_sample.  Conventions as above; a call runs on the device of its
+ * stream (the current one for NULL), and all its buffers are that device's.
+ * ------------------------------------------------------------------------ */
+
+/*
+ * Codes in e4m3 (the OCP format: 4 exponent and 3 mantissa bits, largest value 448) of a
+ * matrix x [rows, cols], with one fp32 scale per group of block_rows x 128 elements
+ * (block_rows 1: hidden states, 128: weights; the last group of a row or column of groups
+ * may be short):
+ *   scale [ceil(rows / block_rows), ceil(cols / 128)] = max |x| / 448 of the group, at
+ *         least 2^-126;
+ *   q     [rows, cols] bytes: x / scale rounded to the nearest code, ties to even.
+ * A group that holds a NaN or an infinity gets the scale NaN and codes 0.  x is fp32 or
+ * bf16 (dtype); cols is a multiple of 16, x and q are 16-byte aligned.  rows = 0 does
+ * nothing.  Needs no workspace.
+ */
+int dcd_quantize_fp8(int64_t rows, int32_t cols, int32_t dtype, int32_t block_rows, const void *x, void *q,
+                     float *scale, void *hip_stream);
+
+typedef struct {
+    int32_t rows;         /* rows of hidden states, >= 0 (0: the call does nothing)             */
+    int32_t vocab;        /* V >= 1                                                      */
+    int32_t hidden;       /* d >= 16, a multiple of 16                                   */
+    int32_t dtype;        /* of the logits: DCD_F32 or DCD_BF16                          */
+    int64_t stride;       /* elements from one row of logits to the next, >= V; 0 = V    */
+} dcd_fp8_problem;
+
+typedef struct {               /* device pointers, read only                               */
+    const void *h;             /* [rows, d] e4m3 codes, 16-byte aligned                     */
+    const float *h_scale;      /* [rows, ceil(d / 128)]                                     */
+    const void *w;             /* [V, d] e4m3 codes, 16-byte aligned                        */
+    const float *w_scale;      /* [ceil(V / 128), ceil(d / 128)]                            */
+    const float *bias;         /* [V] fp32 logit bias, or NULL for none                     */
+} dcd_fp8_inputs;
+
+/*
+ * Logits of a head held in 8 bits:
+ *   z[r, v] = sum over blocks b of 128 columns of
+ *               h_scale[r, b] * w_scale[v / 128, b] * sum_{k in b} h[r, k] w[v, k]  + bias[v]
+ * with exact products, fp32 sums, and one rounding at the end for bf16 logits.  Elements
+ * of `logits` between V and the row stride are left as they were.  Needs no workspace.
+ */
+int dcd_logits_fp8(const dcd_fp8_problem *p, const dcd_fp8_inputs *in, void *logits, void *hip_stream);
+
+typedef struct {
+    int32_t rows;         /* >= 0 (0: the call does nothing)                              */
+    int32_t vocab;        /* V >= 1                                                      */
+    int32_t dtype;        /* of the logits: DCD_F32 or DCD_BF16                          */
+    int64_t stride;       /* elements from one row of logits to the next, >= V; 0 = V    */
+} dcd_sample_problem;
+
+typedef struct {               /* device pointers, read only; each rule is one value per row */
+    const void *logits;        /* [rows, stride], aligned to its element; -inf: masked token */
+    const float *u;            /* [rows] uniforms in [0, 1)                                  */
+    const float *temperature;  /* [rows] T >= 0, or NULL for 1; 0: the row's argmax          */
+    const int32_t *top_k;      /* [rows], or NULL for off; <= 0 or > V: off                  */
+    const float *top_p;        /* [rows] in [0, 1], or NULL for off; 1: off                  */
+    const float *min_p;        /* [rows] in [0, 1], or NULL for off; 0: off                  */
+} dcd_sample_inputs;
+
+typedef struct {               /* device pointers, written by the call                       */
+    int32_t *tokens;           /* [rows] the token drawn                                     */
+    float *probs;              /* [rows, V] optional: the distribution it was drawn from      */
+    float *logprob;            /* [rows] optional: log of the token's probability in it       */
+    int32_t *kept;             /* [rows] optional: tokens the rules kept                      */
+} dcd_sample_outputs;
+
+/*
+ * A token per row of logits.  Per row, with the tokens ordered by logit (descending; the
+ * lower id first on ties) and weights w = exp((z - max z) / T): the first top_k tokens are
+ * kept; of those the smallest first part whose weights sum to at least top_p times the sum
+ * over the top_k; of those the ones with w >= min_p (of the largest probability).  At
+ * least one token is kept, -inf never.  The token is drawn from the kept weights by inverse
+ * CDF in token-id order: the smallest token whose cumulative weight exceeds u times the
+ * total.  probs is w over that total, 0 for what was not kept.  Weights and their sums are
+ * held in 64 bits.
+ * A row with a NaN or +inf logit, with no finite logit, or with a rule or uniform outside
+ * its range gets token -1, kept 0, logprob NaN and probs 0.
+ * Workspace: device memory of at least dcd_sample_workspace_bytes(p), 256-byte aligned, not
+ * used by any concurrently running call; it need not be cleared.
+ */
+int dcd_sample(const dcd_sample_problem *p, const dcd_sample_inputs *in, const dcd_sample_outputs *out,
+               void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* bytes of device workspace a call with problem `p` needs (0 if `p` is invalid) */
+size_t dcd_sample_workspace_bytes(const dcd_sample_problem *p);
+
 /* static description of a return code (never NULL) */
 const char *dcd_error_string(int code);
 
 /* ABI version of this header: 7 (2: dcd_outputs gained row_argmax_expert and row_kl;
    3: dcd_verify_sample takes trees; 4: dcd_propose; 5: the final RMS normalisation;
-   6: dcd_verify_greedy_noalloc; 7: sequence status DCD_SEQ_WALK_TIMEOUT) */
+   6: dcd_verify_greedy_noalloc; 7: sequence status DCD_SEQ_WALK_TIMEOUT; the 8-bit proposal
+   path came to 7 without a change to what was there) */
 int dcd_abi_version(void);
 
 #ifdef __cplusplus

@@ -24,7 +24,8 @@ NODE_LOGP_P, NODE_LOGP_Q, NODE_CD, NODE_LOGP_CD, NODE_IN_MASK, NODE_RATIO = rang
 
 EXPORTS = ("dcd_workspace_bytes", "dcd_verify_greedy", "dcd_verify_sample",
            "dcd_lmhead_partials", "dcd_propose", "dcd_error_string", "dcd_abi_version",
-           "dcd_verify_greedy_noalloc", "dcd_noalloc_max_bytes")
+           "dcd_verify_greedy_noalloc", "dcd_noalloc_max_bytes", "dcd_quantize_fp8",
+           "dcd_logits_fp8", "dcd_sample", "dcd_sample_workspace_bytes")
 PROBE_EXPORTS = ("dcd_probe_stream_read", "dcd_probe_mfma_bf16")  # include/dcd_probe.h
 
 
@@ -52,6 +53,29 @@ class Outputs(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("accept_len", "accept_path", "next_token", "status",
                                                 "row_argmax", "row_stats", "node_stats",
                                                 "row_argmax_expert", "row_kl")]
+
+
+class Fp8Problem(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("vocab", ctypes.c_int32), ("hidden", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("stride", ctypes.c_int64)]
+
+
+class Fp8Inputs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("h", "h_scale", "w", "w_scale", "bias")]
+
+
+class SampleProblem(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("vocab", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("stride", ctypes.c_int64)]
+
+
+class SampleInputs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("logits", "u", "temperature", "top_k", "top_p",
+                                                "min_p")]
+
+
+class SampleOutputs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("tokens", "probs", "logprob", "kept")]
 
 
 _lib = None
@@ -84,6 +108,16 @@ def lib() -> ctypes.CDLL:
         L.dcd_verify_greedy_noalloc.restype = ctypes.c_int
         L.dcd_noalloc_max_bytes.argtypes = []
         L.dcd_noalloc_max_bytes.restype = ctypes.c_size_t
+        L.dcd_quantize_fp8.argtypes = [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32,
+                                       ctypes.c_int32, P, P, P, P]
+        L.dcd_quantize_fp8.restype = ctypes.c_int
+        L.dcd_logits_fp8.argtypes = [ctypes.POINTER(Fp8Problem), ctypes.POINTER(Fp8Inputs), P, P]
+        L.dcd_logits_fp8.restype = ctypes.c_int
+        L.dcd_sample_workspace_bytes.argtypes = [ctypes.POINTER(SampleProblem)]
+        L.dcd_sample_workspace_bytes.restype = ctypes.c_size_t
+        L.dcd_sample.argtypes = [ctypes.POINTER(SampleProblem), ctypes.POINTER(SampleInputs),
+                                 ctypes.POINTER(SampleOutputs), P, ctypes.c_size_t, P]
+        L.dcd_sample.restype = ctypes.c_int
         L.dcd_error_string.argtypes = [ctypes.c_int]
         L.dcd_error_string.restype = ctypes.c_char_p
         L.dcd_abi_version.argtypes = []
@@ -133,10 +167,13 @@ def _stream(stream) -> int | None:
     return int(stream.cuda_stream)
 
 
+def _dtype(dtype) -> int:
+    return {"bf16": DCD_BF16, "f32": DCD_F32}.get(dtype, dtype)
+
+
 def make_problem(batch, nodes, vocab, d_expert, d_amateur, dtype="bf16", plaus_thresh=0.1,
                  cd_strength=0.5, temperature=1.0, final_norm=False, norm_eps=0.0) -> Problem:
-    dt = {"bf16": DCD_BF16, "f32": DCD_F32}.get(dtype, dtype)
-    return Problem(batch, nodes, vocab, d_expert, d_amateur, dt, plaus_thresh, cd_strength,
+    return Problem(batch, nodes, vocab, d_expert, d_amateur, _dtype(dtype), plaus_thresh, cd_strength,
                    temperature, int(bool(final_norm)), norm_eps)
 
 
@@ -216,3 +253,47 @@ def propose(problem: Problem, inputs: Inputs, u, tokens, probs, argmax, workspac
     _check(lib().dcd_propose(ctypes.byref(problem), ctypes.byref(inputs), ptr(u), ptr(tokens),
                              ptr(probs), ptr(argmax), ptr(workspace), int(workspace_bytes),
                              _stream(stream)))
+
+
+def quantize_fp8(x, q, scale, *, rows, cols, dtype="bf16", block_rows=1, stream=None) -> None:
+    """Enqueue dcd_quantize_fp8: codes q and scales of x [rows, cols]."""
+    _check(lib().dcd_quantize_fp8(int(rows), int(cols), _dtype(dtype), int(block_rows), ptr(x), ptr(q),
+                                  ptr(scale), _stream(stream)))
+
+
+def make_fp8_problem(rows, vocab, hidden, dtype="f32", stride=0) -> Fp8Problem:
+    return Fp8Problem(rows, vocab, hidden, _dtype(dtype), stride)
+
+
+def make_fp8_inputs(h, h_scale, w, w_scale, bias=None) -> Fp8Inputs:
+    return Fp8Inputs(*(ptr(a) for a in (h, h_scale, w, w_scale, bias)))
+
+
+def logits_fp8(problem: Fp8Problem, inputs: Fp8Inputs, logits, stream=None) -> None:
+    """Enqueue dcd_logits_fp8: the logits of a head held in 8 bits."""
+    _check(lib().dcd_logits_fp8(ctypes.byref(problem), ctypes.byref(inputs), ptr(logits),
+                                _stream(stream)))
+
+
+def make_sample_problem(rows, vocab, dtype="f32", stride=0) -> SampleProblem:
+    return SampleProblem(rows, vocab, _dtype(dtype), stride)
+
+
+def make_sample_inputs(logits, u, temperature=None, top_k=None, top_p=None,
+                       min_p=None) -> SampleInputs:
+    return SampleInputs(*(ptr(a) for a in (logits, u, temperature, top_k, top_p, min_p)))
+
+
+def make_sample_outputs(tokens, probs=None, logprob=None, kept=None) -> SampleOutputs:
+    return SampleOutputs(*(ptr(a) for a in (tokens, probs, logprob, kept)))
+
+
+def sample_workspace_bytes(problem: SampleProblem) -> int:
+    return int(lib().dcd_sample_workspace_bytes(ctypes.byref(problem)))
+
+
+def sample(problem: SampleProblem, inputs: SampleInputs, outputs: SampleOutputs, workspace,
+           workspace_bytes: int, stream=None) -> None:
+    """Enqueue dcd_sample: a token (and its distribution) per row of logits."""
+    _check(lib().dcd_sample(ctypes.byref(problem), ctypes.byref(inputs), ctypes.byref(outputs),
+                            ptr(workspace), int(workspace_bytes), _stream(stream)))

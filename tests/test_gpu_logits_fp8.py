@@ -1,0 +1,150 @@
+"""dcd_logits_fp8 against the definition in 64 bits.
+
+Tolerance: products of two e4m3 codes are exact in fp32; a sum of up to 128 of them, each
+partial sum rounded (or cut off) to fp32, is within 128 * 2^-23 of the magnitudes' sum; the
+scales' product and one multiply-add per block add 2^-24 each and groups * 2^-24 for the
+running sum; the bias one more.  So |error| <= (130 + groups) * 2^-23 * (sum of magnitudes
++ |bias|).  bf16 logits add half a step, 2^-8 of the value.
+"""
+import numpy as np
+import pytest
+import torch
+
+import proposal_oracle as oracle
+from paper_2608_12913_amd import dcd
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def _inputs(M, N, K, seed=0, spread=True):
+    rng = np.random.RandomState(seed)
+    h, hs = oracle.quantize((rng.randn(M, K) * 4).astype(np.float32).astype(np.float64), 1)
+    w, ws = oracle.quantize((rng.randn(N, K) / np.sqrt(K)).astype(np.float32).astype(np.float64), 128)
+    if spread:  # scales of very different sizes: a wrong one shows
+        hs = (hs * 2.0 ** rng.randint(-6, 7, hs.shape)).astype(np.float32)
+        ws = (ws * 2.0 ** rng.randint(-6, 7, ws.shape)).astype(np.float32)
+    bias = rng.randn(N).astype(np.float32)
+    return h, hs, w, ws, bias
+
+
+def _dev(*arrays):
+    return [torch.from_numpy(np.ascontiguousarray(a)).to(DEV) for a in arrays]
+
+
+def _run(arrays, M, N, K, dtype, stride=0, bias=True, out=None, stream=None):
+    t = arrays if torch.is_tensor(arrays[0]) else _dev(*arrays)
+    if out is None:
+        out = torch.full((M, stride or N), -77.0, device=DEV,
+                         dtype=torch.bfloat16 if dtype == "bf16" else torch.float32)
+    dcd.logits_fp8(dcd.make_fp8_problem(M, N, K, dtype, stride),
+                   dcd.make_fp8_inputs(*t[:4], t[4] if bias else None), out,
+                   stream or torch.cuda.current_stream())
+    return out
+
+
+def _check(M, N, K, dtype="f32", stride=0, bias=True, seed=0):
+    a = _inputs(M, N, K, seed)
+    out = _run(a, M, N, K, dtype, stride, bias).double().cpu().numpy()
+    z, mag = oracle.logits(*a[:4], a[4].astype(np.float64) if bias else None)
+    tol = (130 + -(-K // 128)) * 2.0 ** -23 * (mag + (np.abs(a[4]) if bias else 0.0))
+    if dtype == "bf16":
+        tol = tol + 2.0 ** -8 * np.abs(z)
+    bad = np.abs(out[:, :N] - z) > tol
+    assert not bad.any(), (np.argwhere(bad)[:5], bad.sum())
+    assert (out[:, N:] == -77.0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M, N, K", [
+    (1, 1, 16), (1, 5, 128), (2, 17, 48), (3, 1000, 144), (8, 1024, 256), (15, 129, 1040), (16, 128, 512),
+    (17, 2049, 384), (31, 500, 2000), (33, 1031, 640), (48, 4099, 256), (64, 3001, 1024), (65, 1000, 512),
+    (100, 777, 400), (127, 2050, 272), (128, 4096, 512), (129, 1500, 4096), (200, 999, 1536), (257, 1100, 528),
+    (300, 300, 8192), (520, 2000, 256), (1000, 515, 384)])
+def test_sizes(M, N, K, dtype):
+    _check(M, N, K, dtype)
+
+
+@pytest.mark.parametrize("M", [1, 16, 64, 150])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_strides_and_no_bias(M, dtype):
+    _check(M, 1001, 256, dtype, stride=1024)
+    _check(M, 1001, 256, dtype, stride=1003, bias=False)
+
+
+@pytest.mark.parametrize("M", [1, 7, 64, 130, 300])
+def test_large_vocabulary(M):
+    """Vocabulary and hidden size of a real head, against the product of the decoded codes in
+    64 bits on the GPU."""
+    N, K = 128256 if M < 100 else 32003, 4096
+    gen = torch.Generator(device=DEV).manual_seed(M)
+    h = torch.randint(0, 126, (M, K), generator=gen, device=DEV, dtype=torch.uint8)
+    w = torch.randint(0, 126, (N, K), generator=gen, device=DEV, dtype=torch.uint8)
+    h |= torch.randint(0, 2, h.shape, generator=gen, device=DEV, dtype=torch.uint8) << 7
+    w |= torch.randint(0, 2, w.shape, generator=gen, device=DEV, dtype=torch.uint8) << 7
+    hs = torch.rand(M, K // 128, generator=gen, device=DEV) + 0.5
+    ws = torch.rand(-(-N // 128), K // 128, generator=gen, device=DEV) + 0.5
+    out = _run([h, hs, w, ws, None], M, N, K, "f32", bias=False)
+    table = torch.from_numpy(oracle.decode(np.arange(256, dtype=np.uint8))).to(DEV)
+    z = torch.zeros(M, N, device=DEV, dtype=torch.float64)
+    mag = torch.zeros_like(z)
+    for b in range(K // 128):
+        s = slice(128 * b, 128 * b + 128)
+        hv = table[h[:, s].int()] * hs[:, b, None].double()
+        wv = (table[w[:, s].int()] * ws[:, b].double().repeat_interleave(128)[:N, None]).t().contiguous()
+        z += hv @ wv
+        mag += hv.abs() @ wv.abs()
+    assert bool(((out.double() - z).abs() <= (130 + K // 128) * 2.0 ** -23 * mag).all())
+
+
+def test_exact_integers():
+    """Small integers and scales of one: every sum is exact, so the logits are too."""
+    rng = np.random.RandomState(1)
+    for M, N, K in ((5, 300, 512), (64, 700, 256), (200, 600, 384)):
+        code = {-2: 0xC0, -1: 0xB8, 0: 0, 1: 0x38, 2: 0x40}
+        hi, wi = rng.randint(-2, 3, (M, K)), rng.randint(-2, 3, (N, K))
+        enc = np.vectorize(code.get, otypes=[np.uint8])
+        a = (enc(hi), np.ones((M, -(-K // 128)), np.float32), enc(wi),
+             np.ones((-(-N // 128), -(-K // 128)), np.float32), np.zeros(N, np.float32))
+        out = _run(a, M, N, K, "f32").cpu().numpy()
+        assert np.array_equal(out, hi @ wi.T)
+
+
+@pytest.mark.parametrize("M", [4, 64, 140])
+def test_nan_stays_in_its_row_and_token(M):
+    """A row whose scale is NaN, and a token whose code is NaN, make their own logits NaN only."""
+    N, K = 700, 400
+    a = _inputs(M, N, K, 3)
+    clean = _run(a, M, N, K, "f32").cpu().numpy()
+    a[1][1, 2] = np.nan
+    a[2][300, 17] = 0x7F
+    out = _run(a, M, N, K, "f32").cpu().numpy()
+    hit = np.zeros((M, N), bool)
+    hit[1, :] = hit[:, 300] = True
+    assert np.isnan(out[hit]).all()
+    assert np.array_equal(out[~hit], clean[~hit])
+
+
+@pytest.mark.parametrize("M", [1, 40, 64, 180])
+def test_rows_do_not_depend_on_the_batch_size_calls_repeat_and_replay(M):
+    """Bit-identical repeats, on another stream and replayed from a graph with new inputs."""
+    N, K = 5003, 1040
+    t = _dev(*_inputs(M, N, K, 4))
+    first = _run(t, M, N, K, "f32")
+    assert torch.equal(first, _run(t, M, N, K, "f32"))
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(st):
+        other = _run(t, M, N, K, "f32", stream=st)
+    st.synchronize()
+    assert torch.equal(first, other)
+    out = torch.empty_like(first)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        _run(t, M, N, K, "f32", out=out, stream=torch.cuda.current_stream())
+    for seed in (5, 6, 7):
+        for dst, src in zip(t, _dev(*_inputs(M, N, K, seed))):
+            dst.copy_(src)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, _run(t, M, N, K, "f32"))
