@@ -2,10 +2,9 @@
 //   z[r, v] = sum_b hs[r, b] ws[v / 128, b] sum_{k in block b} h[r, k] w[v, k] + bias[v]
 // with e4m3 codes and fp32 scales per 128 columns (and, of the weights, 128 tokens).
 //
-// The codes are widened to bf16 in registers (exactly) and multiplied there.  The 8-bit matrix
-// instructions of gfx950 would align the eight products of a group of columns before they add
-// them, and drop what lies 13 bits below the largest one's power of two: measured, 2^-12
-// of the magnitudes' sum, ten thousand times a rounding to fp32.
+// Up to 64 rows here, more in logits_fp8_tile.hip.  The codes are widened to bf16 in registers
+// (exactly) and multiplied there: the weight stream leaves the matrix cores the time, and their
+// 8-bit instructions lose bits (there).
 //
 // A = weights (tokens), B = hidden states (rows), so a lane's four results belong to one row
 // and the block's scale is one number per lane and row block.  Each block's product starts
@@ -14,136 +13,10 @@
 // the columns will do that is the same for both.
 #include <type_traits>
 
-#include "proposal.h"
+#include "logits_fp8.h"
 
 namespace dcd {
 namespace {
-
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-
-// 32 columns of a block (a lane's 16 + 16) as four operands in bf16.
-struct Wide {
-    bf16x8 v[4];
-    __device__ __forceinline__ void set(const u32x4 &x0, const u32x4 &x1) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const u32x4 &x = i < 2 ? x0 : x1;
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const uint32_t c = x[2 * (i % 2) + j];
-                const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, 1.f, false);
-                const bf16x2 hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, 1.f, true);
-                v[i][4 * j] = lo[0], v[i][4 * j + 1] = lo[1], v[i][4 * j + 2] = hi[0], v[i][4 * j + 3] = hi[1];
-            }
-        }
-    }
-};
-
-__device__ __forceinline__ f32x4 product(const Wide &a, const Wide &b) {
-    f32x4 c = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v[i], b.v[i], c, 0, 0, 0);
-    return c;
-}
-
-__device__ __forceinline__ uint32_t to_bf16(float f) {  // round to nearest even, NaN stays NaN
-    const uint32_t u = __float_as_uint(f);
-    if ((u & 0x7fffffffu) > 0x7f800000u) return (u >> 16) | 0x40u;
-    return (u + 0x7fffu + ((u >> 16) & 1u)) >> 16;
-}
-
-// Four logits of one row, tokens t .. t+3.
-template <int DT>
-__device__ __forceinline__ void store4(const Fp8Problem &P, int row, int t, f32x4 z, bool wide) {
-    const size_t at = (size_t)row * P.stride + t;
-    if constexpr (DT == kF32) {
-        float *o = (float *)P.out + at;
-        if (wide && t + 3 < P.N) {
-            *reinterpret_cast<f32x4 *>(o) = z;
-        } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (t + j < P.N) o[j] = z[j];
-        }
-    } else {
-        uint16_t *o = (uint16_t *)P.out + at;
-        uint32_t b[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) b[j] = to_bf16(z[j]);
-        if (wide && t + 3 < P.N) {
-            *reinterpret_cast<uint2 *>(o) = make_uint2(b[0] | b[1] << 16, b[2] | b[3] << 16);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (t + j < P.N) o[j] = (uint16_t)b[j];
-        }
-    }
-}
-
-typedef __attribute__((address_space(3))) void *lds_ptr;
-
-// Waits until at most N of this wave's vector memory operations are outstanding (they
-// complete in issue order; the compiler does not track loads that write LDS).
-template <int N>
-__device__ __forceinline__ void wait_loads() {
-    static_assert(N < 64, "vmcnt is 6 bits");
-    __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | (N >> 4) << 14);
-}
-
-// All waves of the workgroup; loads in flight stay so (__syncthreads() would wait for them).
-__device__ __forceinline__ void barrier() {
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-}
-
-// A lane's two 16-byte pieces of a tile, at LDS address `at` and 64 columns on.  One block with
-// its own wait: for plain loads the compiler would wait for every load to LDS in flight.
-__device__ __forceinline__ void read_tile(u32x4 &a0, u32x4 &a1, uint32_t at) {
-    asm volatile("ds_read_b128 %0, %2\n ds_read_b128 %1, %3\n s_waitcnt lgkmcnt(0)"
-                 : "=&v"(a0), "=&v"(a1)
-                 : "v"(at), "v"(at ^ 64u)
-                 : "memory");
-}
-
-__device__ __forceinline__ float read_float(uint32_t at) {
-    float x;
-    asm volatile("ds_read_b32 %0, %1\n s_waitcnt lgkmcnt(0)" : "=&v"(x) : "v"(at) : "memory");
-    return x;
-}
-
-// The same of hidden states, with the row's scale.
-__device__ __forceinline__ void read_rows(u32x4 &a0, u32x4 &a1, float &s, uint32_t at, uint32_t scale_at) {
-    asm volatile("ds_read_b128 %0, %3\n ds_read_b128 %1, %4\n ds_read_b32 %2, %5\n s_waitcnt lgkmcnt(0)"
-                 : "=&v"(a0), "=&v"(a1), "=&v"(s)
-                 : "v"(at), "v"(at ^ 64u), "v"(scale_at)
-                 : "memory");
-}
-
-constexpr int TILE = 16 * kGroup;  // bytes of 16 rows x 128 columns
-
-// Offset of a lane's first piece in such a tile in LDS.  A tile is 16 rows of 128 bytes; the
-// 16-byte column c of row r lies at c ^ (r % 8), so that the 16 rows of a matrix operand fall
-// into different banks.  (Its second piece, 64 columns on, lies at the address with bit 6
-// flipped: tiles start at multiples of 128.)
-__device__ __forceinline__ uint32_t piece_offset() {
-    const int lane = threadIdx.x % 64, n = lane % 16, g = lane / 16;
-    return (uint32_t)(n * kGroup + (g ^ n % 8) * 16);
-}
-
-// Half a tile (8 rows) from memory into LDS: lane l lands at byte 16 l, which holds column
-// (l % 8) ^ (l / 8) of row l / 8.
-template <int AUX>
-__device__ __forceinline__ void load_half(const uint8_t *base, uint32_t off, char *to) {
-    __builtin_amdgcn_global_load_lds(base + off, (lds_ptr)to, 16, 0, AUX);
-}
-
-__device__ __forceinline__ uint32_t lds_address(const char *p) {
-    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)p;
-}
 
 // Geometry of the weight stream for RB blocks of 16 rows and TB tiles of 16 tokens per wave.
 // KS = 1: four waves of different tokens share the hidden states; KS = 4: four waves share
@@ -182,7 +55,7 @@ struct StreamGeo {
 // A vocabulary too small to fill the chip that way takes KS = 4: 16 tokens per workgroup,
 // a quarter of K per wave, the four sums added in their order at the end.
 template <int RB, int TB, int KS, int DT>
-__device__ __forceinline__ void stream_body(const Fp8Problem &P, int wide, char *lds) {
+__device__ __forceinline__ void stream_body(const Fp8Problem &P, char *lds) {
     using G = StreamGeo<RB, TB, KS>;
     constexpr int S = G::SLOTS, HT = G::HT, HL = G::HL;
     const int lane = threadIdx.x % 64, n = lane % 16, g = lane / 16;
@@ -310,15 +183,15 @@ __device__ __forceinline__ void stream_body(const Fp8Problem &P, int wide, char 
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
             const int row = 16 * r + n;
-            if (row < P.M && tok < P.N) store4<DT>(P, row, tok, acc[t][r] + b, wide);
+            if (row < P.M && tok < P.N) store4<DT>(P, row, tok, acc[t][r] + b);
         }
     }
 }
 
 template <int RB, int TB, int KS, int DT>
-__global__ __launch_bounds__(256, KS == 1 ? 2 : 1) void logits_stream_kernel(Fp8Problem P, int wide) {
+__global__ __launch_bounds__(256, KS == 1 ? 2 : 1) void logits_stream_kernel(Fp8Problem P) {
     __shared__ __align__(128) char lds[StreamGeo<RB, TB, KS>::LDS];
-    stream_body<RB, TB, KS, DT>(P, wide, lds);
+    stream_body<RB, TB, KS, DT>(P, lds);
 }
 
 // Two workgroups fit a CU, so tokens per wave (64, 32 or 16) go by what gives the chip's 512
@@ -328,95 +201,30 @@ __global__ __launch_bounds__(256, KS == 1 ? 2 : 1) void logits_stream_kernel(Fp8
 // 4,096, 4096: 52 / 33 / 27 / 12.  One row: 128,256, 4096: 82 / 95 / 91 / 186;
 // 8,192, 2048: 17 / 12 / 10 / 9.
 template <int RB, int DT>
-void launch_stream(const Fp8Problem &p, int wide, hipStream_t st) {
+void launch_stream(const Fp8Problem &p, hipStream_t st) {
     const int tokens = p.N >= 98304 ? 64 : p.N >= 49152 ? 32 : p.N > 12288 ? 16 : 0;
     const dim3 wg(256);
     auto grid = [&](int per) { return dim3((unsigned)((p.N + per - 1) / per)); };
     if (tokens == 64)
-        hipLaunchKernelGGL((logits_stream_kernel<RB, 4, 1, DT>), grid(256), wg, 0, st, p, wide);
+        hipLaunchKernelGGL((logits_stream_kernel<RB, 4, 1, DT>), grid(256), wg, 0, st, p);
     else if (tokens == 32)
-        hipLaunchKernelGGL((logits_stream_kernel<RB, 2, 1, DT>), grid(128), wg, 0, st, p, wide);
+        hipLaunchKernelGGL((logits_stream_kernel<RB, 2, 1, DT>), grid(128), wg, 0, st, p);
     else if (tokens == 16)
-        hipLaunchKernelGGL((logits_stream_kernel<RB, 1, 1, DT>), grid(64), wg, 0, st, p, wide);
+        hipLaunchKernelGGL((logits_stream_kernel<RB, 1, 1, DT>), grid(64), wg, 0, st, p);
     else
-        hipLaunchKernelGGL((logits_stream_kernel<RB, 1, 4, DT>), grid(16), wg, 0, st, p, wide);
-}
-
-// A wave owns 32 tokens x 32 rows.
-template <int DT>
-__global__ __launch_bounds__(256) void logits_rows_kernel(Fp8Problem P, int wide) {
-    constexpr int RB = 2, TB = 2;
-    const int lane = threadIdx.x % 64, n = lane % 16, g = lane / 16;
-    const int tok0 = (blockIdx.x * 4 + threadIdx.x / 64) * 16 * TB, row0 = blockIdx.y * 16 * RB;
-    if (tok0 >= P.N) return;
-    const uint8_t *w[TB], *h[RB];
-    const float *hs[RB];
-#pragma unroll
-    for (int t = 0; t < TB; ++t) w[t] = P.w + (size_t)min(tok0 + 16 * t + n, P.N - 1) * P.K;
-#pragma unroll
-    for (int r = 0; r < RB; ++r) {
-        const int row = min(row0 + 16 * r + n, P.M - 1);
-        h[r] = P.h + (size_t)row * P.K;
-        hs[r] = P.hs + (size_t)row * P.groups;
-    }
-    const float *ws = P.ws + (size_t)(tok0 / kGroup) * P.groups;
-    f32x4 acc[TB][RB] = {};
-    for (int b = 0; b < P.groups; ++b) {
-        u32x4 a[TB][2], x[RB][2];
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const int k = b * kGroup + 64 * s + 16 * g;
-            const bool in = k < P.K;  // K is a multiple of 16
-#pragma unroll
-            for (int t = 0; t < TB; ++t) a[t][s] = in ? *(const u32x4 *)(w[t] + k) : u32x4{0, 0, 0, 0};
-#pragma unroll
-            for (int r = 0; r < RB; ++r) x[r][s] = in ? *(const u32x4 *)(h[r] + k) : u32x4{0, 0, 0, 0};
-        }
-        const float wsb = ws[b];
-        Wide wa[TB], xb[RB];
-#pragma unroll
-        for (int t = 0; t < TB; ++t) wa[t].set(a[t][0], a[t][1]);
-#pragma unroll
-        for (int r = 0; r < RB; ++r) xb[r].set(x[r][0], x[r][1]);
-#pragma unroll
-        for (int r = 0; r < RB; ++r) {
-            const float s = hs[r][b] * wsb;
-#pragma unroll
-            for (int t = 0; t < TB; ++t) {
-                const f32x4 p = product(wa[t], xb[r]);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[t][r][j] = fmaf(p[j], s, acc[t][r][j]);
-            }
-        }
-    }
-#pragma unroll
-    for (int t = 0; t < TB; ++t) {
-        const int tok = tok0 + 16 * t + 4 * g;
-        f32x4 b;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) b[j] = P.bias && tok + j < P.N ? P.bias[tok + j] : 0.f;
-#pragma unroll
-        for (int r = 0; r < RB; ++r) {
-            const int row = row0 + 16 * r + n;
-            if (row < P.M) store4<DT>(P, row, tok, acc[t][r] + b, wide);
-        }
-    }
+        hipLaunchKernelGGL((logits_stream_kernel<RB, 1, 4, DT>), grid(16), wg, 0, st, p);
 }
 
 template <int DT>
 hipError_t launch(const Fp8Problem &p, hipStream_t st) {
-    const int esz = DT == kF32 ? 4 : 2;
-    // rows that start on a multiple of four elements take their stores four at a time
-    const int wide = p.stride % 4 == 0 && (uintptr_t)p.out % (4 * esz) == 0;
     if (p.M <= 16)
-        launch_stream<1, DT>(p, wide, st);
+        launch_stream<1, DT>(p, st);
     else if (p.M <= 32)
-        launch_stream<2, DT>(p, wide, st);
+        launch_stream<2, DT>(p, st);
     else if (p.M <= 64)
-        launch_stream<4, DT>(p, wide, st);
+        launch_stream<4, DT>(p, st);
     else
-        hipLaunchKernelGGL((logits_rows_kernel<DT>), dim3((unsigned)((p.N + 127) / 128), (unsigned)((p.M + 31) / 32)),
-                           dim3(256), 0, st, p, wide);
+        return launch_logits_tile(p, st);
     return hipGetLastError();
 }
 

@@ -32,6 +32,7 @@ struct Fp8Problem {
 };
 
 hipError_t launch_logits_fp8(const Fp8Problem &p, hipStream_t st);
+hipError_t launch_logits_tile(const Fp8Problem &p, hipStream_t st);  // more than 64 rows
 
 struct SampleProblem {
     int R, V, dtype;

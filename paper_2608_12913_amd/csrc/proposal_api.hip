@@ -71,6 +71,8 @@ int run_logits(const dcd_fp8_problem *p, const dcd_fp8_inputs *in, void *logits,
     const int64_t stride = p->stride ? p->stride : p->vocab;
     if (stride < p->vocab || stride > kMaxVocab) return DCD_ERR_SHAPE;
     if (!logit_type(p->dtype)) return DCD_ERR_PARAM;
+    // tiles of 256 tokens x at least 128 rows, 512 threads each, their total counted in 32 bits
+    if (((int64_t)p->vocab / 256 + 9) * (p->rows / 128 + 1) >= 1 << 23) return DCD_ERR_SHAPE;
     if (p->hidden % 16) return DCD_ERR_ALIGN;
     if (p->rows == 0) return DCD_OK;
     if (!in || !in->h || !in->h_scale || !in->w || !in->w_scale || !logits) return DCD_ERR_NULL;
