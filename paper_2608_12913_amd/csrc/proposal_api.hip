@@ -104,6 +104,8 @@ int make_sample(const dcd_sample_problem *p, SampleProblem &P) {
     const int64_t stride = p->stride ? p->stride : p->vocab;
     if (stride < p->vocab || stride > kMaxVocab) return DCD_ERR_SHAPE;
     if (!logit_type(p->dtype)) return DCD_ERR_PARAM;
+    // a launch counts its threads in 32 bits: 1024 per row, 256 per slice of at least 2,048 tokens
+    if (p->rows >= 1 << 22 || ((int64_t)p->vocab / 2048 + 1) * p->rows >= 1 << 24) return DCD_ERR_SHAPE;
     P = SampleProblem{};
     P.R = p->rows;
     P.V = p->vocab;
