@@ -13,14 +13,14 @@
 // up to the same whatever the order, so that sums in LDS atomics give the same bits in every
 // call and a border between two tokens is where 64-bit arithmetic puts it.
 //
-// Two launches, or three.  scan_kernel reads the logits once, in slices of 2,048 or 8,192 spread over the chip:
-// the largest logit of every 64, and where no top-k bounds the row the slice's weight and (top-p) a
-// coarse histogram of it; it writes the zeros of the probabilities.  pick_kernel has a workgroup per
-// row, which brackets the cutoff from these, reads again only the pieces that can hold kept
-// tokens, sorts what lies inside the bracket and draws.  Rows without any rule are not cut: their
-// dense probabilities are one more pass, spread over the chip (whole_kernel).  Where the bracket
-// fails (too many tokens inside, a top-k larger than the number of pieces) the row's workgroup
-// searches the logits themselves (search_row).
+// Two launches, or three.  scan_kernel reads the logits once, in slices of 2,048 or 8,192 spread over
+// the chip: the largest logit of every 64 and, where no top-k bounds the row, a histogram of the
+// slice's weight; it writes the zeros of the probabilities.  pick_kernel has a workgroup per row, which
+// brackets the cutoff from these to a few hundred tokens, reads again only the pieces that can hold
+// one, puts what lies inside the bracket in order, and draws.  What lies surely above the bracket
+// (rows without top-k) is spread over the chip once more for its dense probabilities
+// (spread_kernel).  Where the bracket fails (too many tokens inside, a top-k larger than the
+// number of pieces) the row's workgroup searches the logits themselves (search_row).
 #include "proposal.h"
 
 namespace dcd {
@@ -28,7 +28,7 @@ namespace {
 
 typedef unsigned long long u64;
 
-constexpr int NT = 1024;             // threads of a row's workgroup
+constexpr int NT = 256;              // threads of a row's workgroup
 constexpr int NW = NT / 64;
 constexpr int BITS = 11;             // of a key per search level
 constexpr int BINS = 1 << BITS;
@@ -102,7 +102,7 @@ struct Rules {
         if (k < 0 || k >= P.V) k = 0;
         whole = ok && k == 0 && p == 1.f && m == 0.f;
     }
-    __device__ __forceinline__ bool weighs() const { return ok && k == 0 && (whole || p < 1.f); }  // all of the row
+    __device__ __forceinline__ bool weighs() const { return ok && k == 0; }  // all of the row
 };
 
 // The last kept element of the order.
@@ -429,20 +429,30 @@ constexpr int UNIT = 256;       // logits read again together
 constexpr int HB = 256;         // histogram bins, 1/16 of a temperature wide, below the slice's largest logit
 constexpr int SLICE = 8192;     // logits per slice (of a dense row's second pass, too)
 constexpr int MAXV = 1 << 20;   // largest vocabulary of this path
-constexpr int MAXLIST = 8192;   // tokens inside a row's bracket
+constexpr int MAXLIST = 4096;   // tokens inside a row's bracket
+constexpr int MAXCOUNTED = 512;  // up to so many are put in order by counting
+constexpr int kHistShift = 50;  // 8,192 weights of a slice stay below 2^63
 constexpr int MAXSLICES = MAXV / SLICE > 512 ? MAXV / SLICE : 512;
 constexpr float kBinLimit = 4194304.f;  // |bin numbers| up to here are exact in fp32
 
 struct SliceStat {
     uint32_t top, bad, finite, unused;
-    double mass;  // weight relative to the slice's largest logit
+    u64 mass;  // rows without top-k: the slice's weight, relative to its largest logit, at 2^kHistShift
+};
+
+// What pick_kernel leaves for a row's dense probabilities.
+struct Spread {
+    double scale;    // of a weight
+    uint32_t top;    // key of the row's largest logit
+    uint32_t least;  // every token from this key on is kept (0xffffffff: none)
 };
 
 struct Scan {
     int slice, slices, pieces, units;  // logits per slice; slices, pieces and units of a row
     SliceStat *stat;                   // [R][slices]
     uint32_t *tops;                    // [R][pieces]: key of each piece's largest logit
-    float *hist;                       // [R][slices][HB]
+    u64 *hist;                         // [R][slices][HB]: weights at 2^kHistShift, the last bin: the rest
+    Spread *spread;                    // [R]
 };
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -478,11 +488,34 @@ __device__ __forceinline__ const char *row_of(const SampleProblem &P, int r) {
 // Bin number of a logit: the same in both launches, and monotone.
 __device__ __forceinline__ float bin_of(float z, float per) { return floorf(z * per); }
 
+// Sums along a wave in registers: row shifts within 16 lanes, then broadcasts of a row's last lane.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u64 shifted(u64 x) {
+    const int lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, CTRL, ROWS, 0xf, false);
+    const int hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(x >> 32), CTRL, ROWS, 0xf, false);
+    return (u64)(uint32_t)hi << 32 | (uint32_t)lo;
+}
+__device__ __forceinline__ u64 wave_scan(u64 x) {  // inclusive
+    x += shifted<0x111, 0xf>(x);
+    x += shifted<0x112, 0xf>(x);
+    x += shifted<0x114, 0xf>(x);
+    x += shifted<0x118, 0xf>(x);
+    x += shifted<0x142, 0xa>(x);
+    x += shifted<0x143, 0xc>(x);
+    return x;
+}
+__device__ __forceinline__ u64 last_lane(u64 x) {
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, 63);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(x >> 32), 63);
+    return (u64)hi << 32 | lo;
+}
+__device__ __forceinline__ u64 wave_sum(u64 x) { return last_lane(wave_scan(x)); }
+
 // One slice: EPT logits per thread, held in registers between the maximum and the weights.
 template <int DT, int EPT>
 __global__ __launch_bounds__(ST) void scan_kernel(SampleProblem P, Scan L) {
-    __shared__ double table[64], wmass[ST / 64];
-    __shared__ float hist[HB];
+    __shared__ double table[64];
+    __shared__ u64 hist[HB], wmass[ST / 64];
     __shared__ uint32_t wtop[ST / 64], wbad[ST / 64], wfinite[ST / 64];
     const int s = blockIdx.x % L.slices, r = blockIdx.x / L.slices;
     const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
@@ -507,7 +540,7 @@ __global__ __launch_bounds__(ST) void scan_kernel(SampleProblem P, Scan L) {
     const bool weighs = rules.weighs();
     if (weighs) {
         fill_table(table);
-        hist[tid] = 0.f;
+        hist[tid] = 0;
     }
     uint32_t top = 0, bad = 0, finite = 0;
     uint32_t *tops = L.tops + (size_t)r * L.pieces;
@@ -545,28 +578,27 @@ __global__ __launch_bounds__(ST) void scan_kernel(SampleProblem P, Scan L) {
         bad |= wbad[w];
         finite += wfinite[w];
     }
-    SliceStat st{top, bad, finite, 0, 0.0};
+    SliceStat st{top, bad, finite, 0, 0};
     if (weighs && finite && !bad) {
-        const Weights W{(double)logit_of(top), 1.0 / (double)rules.T, 1.0, table};
+        const Weights W{(double)logit_of(top), 1.0 / (double)rules.T, (double)(1ull << kHistShift), table};
+        u64 m = 0;
         const float per = 16.f / rules.T, first = bin_of(logit_of(top), per);
-        double m = 0.0;
 #pragma unroll
         for (int i = 0; i < EPT / 4; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const uint32_t key = key_of(z[i][j]);
                 if (key < kLowest) continue;
-                const double w = W.exact(key);
+                const u64 w = W.fixed(key);
                 m += w;
-                if (rules.p < 1.f) atomicAdd(&hist[(int)fminf(first - bin_of(z[i][j], per), HB - 1.f)], (float)w);
+                if (!rules.whole && w) atomicAdd(&hist[(int)fminf(first - bin_of(z[i][j], per), HB - 1.f)], w);
             }
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) m += __shfl_xor(m, o);
+        m = wave_sum(m);
         if (lane == 0) wmass[wave] = m;
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < ST / 64; ++w) st.mass += wmass[w];
-        if (rules.p < 1.f) L.hist[((size_t)r * L.slices + s) * HB + tid] = hist[tid];
+        if (!rules.whole) L.hist[((size_t)r * L.slices + s) * HB + tid] = hist[tid];
     }
     if (tid == 0) L.stat[(size_t)r * L.slices + s] = st;
 }
@@ -575,159 +607,93 @@ __global__ __launch_bounds__(ST) void scan_kernel(SampleProblem P, Scan L) {
 struct PickLds {
     double table[64];
     union {
-        u64 list[MAXLIST];               // (key, ~id) of the tokens inside the bracket
-        uint32_t tops[2 * MAXLIST];      // before: the pieces' maxima
+        u64 list[MAXLIST + MAXCOUNTED];  // (key, ~id) of the tokens inside the bracket; the last ones: in order
         SearchLds search;                // instead: the search of the logits themselves
     };
-    u64 unit[MAXV / UNIT];               // kept weight per unit
-    uint16_t todo[MAXV / UNIT];          // units that may hold kept tokens
-    float bins[HB], scale[MAXSLICES];
-    int below[MAXSLICES];                // bins from the row's first to the slice's first
-    u64 wmass[NW];
-    uint32_t wcount[NW];
-    u64 total, at, sure_mass;
-    uint32_t top, bad, finite, ntodo, nlist, nsure, pick, lo_bin, hi_bin;
+    uint16_t todo[MAXV / UNIT];  // units that may hold tokens of the bracket
+    double scale[MAXSLICES];     // a slice's largest weight
+    int below[MAXSLICES];        // bins from the row's first to the slice's first
+    u64 kept[MAXSLICES];         // kept weight per slice
+    u64 unit[SLICE / UNIT];      // and per unit of a slice, with the number of its last kept token + 1
+    uint32_t last[SLICE / UNIT];
+    u64 wave[2][NW];             // of block_scan
+    u64 at;
+    uint32_t top[NW], bad[NW], finite[NW];
+    uint32_t ntodo, nlist, pick, lo_bin, hi_bin;
 };
-static_assert(sizeof(PickLds) <= 160 * 1024 && MAXV / PIECE <= 2 * MAXLIST, "LDS of a row");
+static_assert(sizeof(PickLds) <= 64 * 1024, "two rows and more share a CU");
 
-// Exclusive sums over the workgroup of (count, mass), in thread order.
-__device__ __forceinline__ void block_scan(PickLds &S, uint32_t &c, u64 &m) {
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const uint32_t c0 = c;
-    const u64 m0 = m;
+// Exclusive sums over the workgroup in thread order, and the total.  Calls take the two buffers in
+// turns, so that one barrier each is enough: a buffer is written again only after the barrier of the
+// call in between, which everybody reaches with the earlier one read.
+struct BlockScan {
+    PickLds &S;
+    int turn = 0;
+    __device__ __forceinline__ u64 operator()(u64 x, u64 &total) {
+        const int wave = threadIdx.x / 64;
+        const u64 in = wave_scan(x);
+        if (threadIdx.x % 64 == 63) S.wave[turn][wave] = in;
+        __syncthreads();
+        u64 before = 0;
+        total = 0;
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t cc = __shfl_up(c, o);
-        const u64 mm = shfl_up64(m, o);
-        if (lane >= o) {
-            c += cc;
-            m += mm;
+        for (int w = 0; w < NW; ++w) {
+            const u64 y = S.wave[turn][w];
+            before += w < wave ? y : 0;
+            total += y;
         }
+        turn ^= 1;
+        return before + in - x;
     }
-    __syncthreads();
-    if (lane == 63) {
-        S.wcount[wave] = c;
-        S.wmass[wave] = m;
+    __device__ __forceinline__ u64 sum(u64 x) {
+        u64 total;
+        (*this)(x, total);
+        return total;
     }
-    __syncthreads();
-    c -= c0;
-    m -= m0;
-    for (int w = 0; w < wave; ++w) {
-        c += S.wcount[w];
-        m += S.wmass[w];
-    }
-}
-__device__ __forceinline__ u64 block_sum(PickLds &S, u64 m) {
-    uint32_t c = 0;
-    const u64 mine = m;
-    block_scan(S, c, m);
-    if (threadIdx.x == NT - 1) S.total = m + mine;
-    __syncthreads();
-    return S.total;
-}
-
-// A row's largest logit and whether it has a target; with `weigh` the fixed-point weight of each slice
-// in the thread of its number (the others: 0).
-__device__ __forceinline__ bool gather_stats(PickLds &S, const Scan &L, int r, const Rules &rules, int shift, Weights &W,
-                                             u64 &mine) {
-    const int tid = threadIdx.x;
-    if (tid == 0) S.top = S.bad = S.finite = 0;
-    fill_table(S.table);
-    __syncthreads();
-    SliceStat st{0, 0, 0, 0, 0.0};
-    if (tid < L.slices) st = L.stat[(size_t)r * L.slices + tid];
-    if (tid < L.slices) {
-        atomicMax(&S.top, st.top);
-        if (st.bad) atomicOr(&S.bad, 1u);
-        atomicAdd(&S.finite, st.finite);
-    }
-    __syncthreads();
-    W = Weights{(double)logit_of(S.top), 1.0 / (double)rules.T, (double)(1ull << shift), S.table};
-    mine = 0;
-    if (S.bad || !rules.ok || S.top < kLowest) return false;
-    if (rules.weighs() && st.finite) {
-        const double scale = W.exact(st.top);
-        mine = W.to_fixed(st.mass * scale);
-        if (rules.p < 1.f) {
-            const float per = 16.f / rules.T, d = bin_of((float)W.top, per) - bin_of(logit_of(st.top), per);
-            S.scale[tid] = (float)scale;
-            S.below[tid] = (int)fminf(d, (float)HB);
-        }
-    } else if (tid < L.slices) {
-        S.scale[tid] = 0.f;
-        S.below[tid] = HB;
-    }
-    return true;
-}
+};
 
 __device__ __forceinline__ float log_of(const Weights &W, uint32_t key, u64 total) {
     return (float)(((double)logit_of(key) - W.top) * W.inv_T - log((double)total / W.one));
 }
 
-// The draw of a row without rules: the slice where the running weight exceeds the target, then
-// the token in it.
-template <int DT>
-__device__ __forceinline__ void whole_draw(const SampleProblem &P, const Scan &L, int r, const Rules &rules,
-                                           const Weights &W, u64 mine, PickLds &S) {
+// Descending order of n numbers of list[], into list[MAXLIST ..] (few: each by counting the larger ones)
+// or in place.  Returns where.
+__device__ __forceinline__ u64 *sort_list(u64 *list, int n) {
     const int tid = threadIdx.x;
-    const u64 total = block_sum(S, mine);
-    const u64 target = (u64)((double)rules.u * (double)total);  // exceeds: > floor
-    uint32_t none = 0;
-    u64 m = mine;
-    block_scan(S, none, m);
-    if (m <= target && m + mine > target) {
-        S.pick = tid;
-        S.at = m;
-    }
-    __syncthreads();
-    const int per = L.slice / NT, e0 = (int)S.pick * L.slice + tid * per;
-    const char *row = row_of<DT>(P, r);
-    const u64 at = S.at;
-    m = 0;
-    // the slice's last token (of any weight, if there is one), should rounding leave the target above them all
-    constexpr uint32_t kWeighs = 0x80000000u;
-    uint32_t last = 0;
-    for (int j = 0; j < per; ++j) {
-        const uint32_t key = e0 + j < P.V ? key_of(load<DT>(row, e0 + j)) : 0;
-        if (key < kLowest) continue;
-        const u64 w = W.fixed(key);
-        m += w;
-        last = max(last, (uint32_t)(e0 + j) | (w ? kWeighs : 0u));
-    }
-    __syncthreads();
-    if (tid == 0) S.pick = 0;
-    __syncthreads();
-    atomicMax(&S.pick, last);
-    const u64 own = m;
-    block_scan(S, none, m);
-    m += at;
-    if (tid == 0) S.ntodo = S.pick & ~kWeighs;
-    __syncthreads();
-    if (m <= target && m + own > target) {
-        for (int j = 0; j < per; ++j) {
-            const uint32_t key = e0 + j < P.V ? key_of(load<DT>(row, e0 + j)) : 0;
-            if (key >= kLowest) m += W.fixed(key);
-            if (m > target) {
-                S.ntodo = e0 + j;
-                break;
-            }
+    if (n <= MAXCOUNTED) {
+        // each number against the list or a share of it; its place is kept in list[MAXLIST / 2 ..]
+        int size = 64;
+        while (size < n) size <<= 1;
+        const int shares = size < NT ? NT / size : 1, len = size / shares;
+        uint32_t *place = reinterpret_cast<uint32_t *>(list + MAXLIST / 2);
+        for (int e = tid; e < size; e += NT) {
+            place[e] = 0;
+            if (e >= n) list[e] = 0;
         }
+        __syncthreads();
+        for (int e = tid % size; e < size; e += NT) {
+            const int first = size < NT ? tid / size * len : 0;
+            const u64 x = list[e];
+            uint32_t larger = 0;
+            for (int i = first; i < first + len; i += 4) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) larger += list[i + j] > x;
+            }
+            if (e < n) atomicAdd(&place[e], larger);
+        }
+        __syncthreads();
+        for (int e = tid; e < n; e += NT) list[MAXLIST + place[e]] = list[e];
+        __syncthreads();
+        return list + MAXLIST;
     }
+    int size = 1024;
+    while (size < n) size <<= 1;
+    for (int i = n + tid; i < size; i += NT) list[i] = 0;
     __syncthreads();
-    if (tid == 0) {
-        const int token = (int)S.ntodo;
-        P.tokens[r] = token;
-        if (P.logprob) P.logprob[r] = log_of(W, key_of(load<DT>(row, token)), total);
-        if (P.kept) P.kept[r] = (int32_t)S.finite;
-    }
-}
-
-// Descending order of n numbers in LDS (n a power of two, at least 128).  Pairs up to 64 apart stay
-// within a wave.
-__device__ __forceinline__ void sort_list(u64 *list, int n) {
-    for (int k = 2; k <= n; k <<= 1)
+    // pairs up to 64 apart stay within a wave
+    for (int k = 2; k <= size; k <<= 1)
         for (int j = k >> 1; j > 0; j >>= 1) {
-            for (int t = threadIdx.x; t < n / 2; t += NT) {
+            for (int t = tid; t < size / 2; t += NT) {
                 const int i = 2 * j * (t / j) + t % j;
                 const u64 a = list[i], b = list[i + j];
                 if ((a < b) == ((i & k) == 0)) {
@@ -743,283 +709,427 @@ __device__ __forceinline__ void sort_list(u64 *list, int n) {
             }
         }
     __syncthreads();
+    return list;
+}
+
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+
+// The smallest key whose bin is at least b (above every logit's: none).  A wave tries 64 keys around
+// the quotient, which is off by its rounding; where that does not decide (quotients that underflow)
+// it halves the range of all keys.
+__device__ __forceinline__ uint32_t first_key(float b, float per) {
+    constexpr uint32_t kNone = 0xff800000u;
+    const uint32_t from = min(max(key_of(b / per), kLowest + 32u), kNone - 64u) - 32u;
+    const u64 votes = __ballot(bin_of(logit_of(from + threadIdx.x % 64), per) >= b);
+    if (votes && !(votes & 1)) return from + (uint32_t)__ffsll((long long)votes) - 1;
+    uint32_t lo = kLowest, hi = kNone;
+    while (lo < hi) {
+        const uint32_t mid = lo + (hi - lo) / 2;
+        if (bin_of(logit_of(mid), per) >= b)
+            hi = mid;
+        else
+            lo = mid + 1;
+    }
+    return lo;
 }
 
 // A row's token.
 template <int DT>
 __device__ void pick_row(const SampleProblem &P, const Scan &L, int r, int shift, int idbits, PickLds &S) {
     const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
-    const Rules rules(P, r);
     const char *row = row_of<DT>(P, r);
-    Weights W;
-    u64 mine;
-    if (!gather_stats(S, L, r, rules, shift, W, mine)) {
-        if (tid == 0) no_token(P, r);
+    BlockScan scan{S};
+    // everything that is read at an address known from the start: one trip to memory
+    constexpr int SPT = MAXSLICES / NT;  // slices per thread
+    SliceStat st[SPT];
+#pragma unroll
+    for (int i = 0; i < SPT; ++i) {
+        st[i] = SliceStat{0, 0, 0, 0, 0};
+        if (tid + i * NT < L.slices) st[i] = L.stat[(size_t)r * L.slices + tid + i * NT];
+    }
+    constexpr int MOST = MAXV / UNIT / NT;  // units per thread
+    u32x4 tops[MOST];
+    const u32x4 *all_tops = reinterpret_cast<const u32x4 *>(L.tops + (size_t)r * L.pieces);
+#pragma unroll
+    for (int i = 0; i < MOST; ++i) {
+        tops[i] = u32x4{0, 0, 0, 0};
+        if (tid + i * NT < L.units) tops[i] = all_tops[tid + i * NT];
+    }
+    const Rules rules(P, r);
+    fill_table(S.table);
+    // the row's largest logit
+    uint32_t top = 0, finite = 0, bad = 0;
+#pragma unroll
+    for (int i = 0; i < SPT; ++i) {
+        top = max(top, st[i].top);
+        finite += st[i].finite;
+        bad |= st[i].bad;
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
+    finite = (uint32_t)wave_sum(finite);
+    const u64 bads = __ballot(bad != 0);
+    if (lane == 0) {
+        S.top[wave] = top;
+        S.finite[wave] = finite;
+        S.bad[wave] = bads != 0;
+    }
+    if (tid == 0) {
+        S.ntodo = S.nlist = 0;
+        S.lo_bin = S.hi_bin = HB;
+    }
+    __syncthreads();
+    bad = top = finite = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        top = max(top, S.top[w]);
+        bad |= S.bad[w];
+        finite += S.finite[w];
+    }
+    Spread spread{0.0, top, 0xffffffffu};
+    if (bad || !rules.ok || top < kLowest) {
+        if (tid == 0) {
+            L.spread[r] = spread;
+            no_token(P, r);
+        }
         return;
     }
-    if (rules.whole) {
-        whole_draw<DT>(P, L, r, rules, W, mine, S);
-        return;
+    const Weights W{(double)logit_of(top), 1.0 / (double)rules.T, (double)(1ull << shift), S.table};
+    const float per = 16.f / rules.T, first = bin_of((float)W.top, per);
+    if (rules.k == 0) {
+#pragma unroll
+        for (int i = 0; i < SPT; ++i) {
+            const int s = tid + i * NT;
+            if (s >= L.slices) break;
+            S.scale[s] = st[i].finite ? W.exact(st[i].top) : 0.0;
+            S.below[s] = st[i].finite ? (int)fminf(first - bin_of(logit_of(st[i].top), per), (float)HB) : HB;
+            S.kept[s] = 0;
+        }
+    } else {
+        for (int s = tid; s < L.slices; s += NT) S.kept[s] = 0;
     }
     auto search = [&] {
         __syncthreads();
+        if (tid == 0) L.spread[r] = Spread{0.0, top, 0xffffffffu};
         search_row<DT>(P, r, rules, shift, idbits, S.search, S.table);
     };
-    // The bracket: tokens that are surely kept by top-k and top-p, and the ones that may be.  By
-    // logit (key >= least) or by histogram bin (from hi_bin on sure, from lo_bin on possible; min-p is
-    // decided token by token).
-    const int k = min(rules.k, (int)S.finite);
-    const bool bins = rules.k == 0 && rules.p < 1.f, all_sure = rules.k == 0 && !bins;
-    uint32_t least = kLowest;
-    float per = 0.f, lo = 0.f, hi = 0.f;
-    u64 total = 0;
-    const uint32_t *tops = L.tops + (size_t)r * L.pieces;
-    if (tid == 0) S.ntodo = S.nlist = S.nsure = S.sure_mass = 0;
-    if (bins) {
-        total = block_sum(S, mine);
-        per = 16.f / rules.T;
-        const float first = bin_of((float)W.top, per);
+    // The bracket: tokens with key >= high are surely kept, those with key >= low may be.
+    const int k = min(rules.k, (int)finite);
+    uint32_t low = kLowest, high = 0xffffffffu;
+    u64 total = 0, goal = 0, sure_mass = 0;
+    bool bounded = false;  // the bracket ends where min-p does: top-p need not cut inside it
+    auto to_row = [&](u64 x, int s) {  // a slice's weight in the row's fixed point
+        return (u64)rint((double)x * S.scale[s] * (W.one / (double)(1ull << kHistShift)));
+    };
+    if (rules.whole) {
+        high = kLowest;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < SPT; ++i)
+            if (tid + i * NT < L.slices) S.kept[tid + i * NT] = to_row(st[i].mass, tid + i * NT);
+    } else if (rules.k == 0) {
         if (!(fabsf(first) < kBinLimit)) return search();
-        // the row's histogram, in units of its largest weight, and its running sum
-        float h = 0.f;
-        if (tid < HB)
-            for (int s = 0; s < L.slices; ++s) {
-                const int b = tid - S.below[s];
-                if (b >= 0 && b < HB - 1) h += L.hist[((size_t)r * L.slices + s) * HB + b] * S.scale[s];
+        __syncthreads();
+        u64 mine = 0;
+#pragma unroll
+        for (int i = 0; i < SPT; ++i)
+            if (tid + i * NT < L.slices) mine += to_row(st[i].mass, tid + i * NT);
+        total = scan.sum(mine);
+        // the row's histogram, a bin per thread, and its running sum
+        const u64 *hist = L.hist + (size_t)r * L.slices * HB;
+        constexpr int AHEAD = 8;
+        u64 h = 0;
+        for (int s0 = 0; s0 < L.slices; s0 += AHEAD) {
+            u64 x[AHEAD];
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                const int s = min(s0 + i, L.slices - 1), b = s0 + i < L.slices ? tid - S.below[s] : -1;
+                x[i] = b >= 0 && b < HB - 1 ? hist[(size_t)s * HB + b] : 0;
             }
-        if (tid < HB) S.bins[tid] = h;
-        __syncthreads();
-        for (int o = 1; o < HB; o <<= 1) {
-            const float x = tid >= o && tid < HB ? S.bins[tid - o] : 0.f;
-            __syncthreads();
-            if (tid < HB) S.bins[tid] += x;
-            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i)
+                if (x[i]) h += to_row(x[i], min(s0 + i, L.slices - 1));
         }
-        if (tid == 0) S.lo_bin = S.hi_bin = HB;
-        __syncthreads();
-        // the sums in fp32 are good to far better than a thousandth
-        const float goal = (float)((double)rules.p * ((double)total / W.one));
-        if (tid < HB - 1) {
-            if (S.bins[tid] * 1.001f >= goal) atomicMin(&S.hi_bin, (uint32_t)tid);
-            if (S.bins[tid] * 0.999f >= goal) atomicMin(&S.lo_bin, (uint32_t)tid);
+        u64 all;
+        const u64 before = scan(h, all), run = before + h;
+        int lo_bin = HB, hi_bin = HB;
+        if (rules.p < 1.f) {
+            goal = (u64)ceil((double)rules.p * (double)total);
+            goal = goal < 1 ? 1 : goal > total ? total : goal;
+            // (slices and bins were rounded apart: a billionth is far more than that)
+            if (tid < HB - 1) {
+                if ((double)run >= (double)goal * (1.0 - 1e-9)) atomicMin(&S.hi_bin, (uint32_t)tid);
+                if ((double)run >= (double)goal * (1.0 + 1e-9)) atomicMin(&S.lo_bin, (uint32_t)tid);
+            }
+            __syncthreads();
+            hi_bin = (int)S.hi_bin;
+            lo_bin = (int)S.lo_bin;
+        }
+        if (rules.m > 0.f) {  // the bins around the logit of weight min_p
+            const double z = W.top + (double)rules.T * log((double)rules.m), d = fabs(z) * 1e-6 + 1e-30;
+            const float above = first - bin_of((float)(z + d), per), under = first - bin_of((float)(z - d), per);
+            hi_bin = min(hi_bin, (int)fmaxf(fminf(above, (float)HB), 0.f));
+            if (under < (float)lo_bin) {
+                lo_bin = (int)fmaxf(under, 0.f);
+                bounded = true;
+            }
+        }
+        if (lo_bin >= HB - 1) return search();
+        low = first_key(first - (float)lo_bin, per);
+        high = first_key(first - (float)hi_bin + 1.f, per);
+        if (tid == hi_bin) S.at = before;
+        // the sure weight per slice
+        for (int s0 = wave; s0 < L.slices; s0 += NW * 4) {
+            u64 x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int s = min(s0 + i * NW, L.slices - 1), most = min(hi_bin - S.below[s], HB - 1);
+                x[i] = 0;
+#pragma unroll
+                for (int j = 0; j < HB / 64; ++j)
+                    if (lane + 64 * j < most) x[i] += hist[(size_t)s * HB + lane + 64 * j];
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int s = s0 + i * NW;
+                if (s >= L.slices) break;
+                const u64 y = wave_sum(x[i]);
+                if (lane == 0) S.kept[s] = to_row(y, s);
+            }
         }
         __syncthreads();
-        if (S.lo_bin >= HB - 1) return search();
-        lo = first - (float)S.lo_bin;
-        hi = first - (float)S.hi_bin;
-    } else if (all_sure) {
-        // the logit of weight min_p, a little lower
-        const double z = W.top + (double)rules.T * log((double)rules.m);
-        const float f = (float)(z - fabs(z) * 1e-6 - 1e-30);
-        least = f >= -3.4028235e38f ? max(key_of(f), kLowest) : kLowest;
+        sure_mass = S.at;
     } else if (k <= L.pieces) {
         // at least k tokens reach the k-th largest of the pieces' maxima; its upper 16 bits do
-        for (int i = tid; i < L.pieces; i += NT) S.tops[i] = tops[i];
-        __syncthreads();
         uint32_t prefix = 0;
         for (int bit = 30; bit >= 16; bit -= 2) {
             u64 counts = 0;
-            for (int i = tid; i - tid < L.pieces; i += NT) {
-                const uint32_t key = i < L.pieces ? S.tops[i] : 0;
 #pragma unroll
-                for (int c = 1; c < 4; ++c)
-                    counts += (u64)__popcll(__ballot(i < L.pieces && key >= (prefix | (uint32_t)c << bit))) << (21 * (c - 1));
-            }
-            __syncthreads();
-            if (lane == 0) S.wmass[wave] = counts;
+            for (int i = 0; i < MOST; ++i)
+                if (i * NT < L.units) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int c = 1; c < 4; ++c)
+                            counts += (u64)__popcll(__ballot(tops[i][j] >= (prefix | (uint32_t)c << bit))) << (21 * (c - 1));
+                }
+            if (lane == 0) S.wave[scan.turn][wave] = counts;
             __syncthreads();
             counts = 0;
 #pragma unroll
-            for (int w = 0; w < NW; ++w) counts += S.wmass[w];
-            for (int c = 3; c > 0; --c)
-                if ((int)(counts >> (21 * (c - 1)) & 0x1fffff) >= k) {
-                    prefix |= (uint32_t)c << bit;
-                    break;
-                }
+            for (int w = 0; w < NW; ++w) counts += S.wave[scan.turn][w];
+            scan.turn ^= 1;
+            int c = 3;
+            while (c > 0 && (int)(counts >> (21 * (c - 1)) & 0x1fffff) < k) --c;
+            prefix |= (uint32_t)c << bit;
         }
-        least = max(prefix, kLowest);
+        low = max(prefix, kLowest);
     }
-    auto possible = [&](uint32_t key) { return key >= least && (!bins || bin_of(logit_of(key), per) >= lo); };
-    auto sure = [&](uint32_t key) { return all_sure || (bins && bin_of(logit_of(key), per) > hi); };
-    // units that hold possible tokens
-    __syncthreads();
-    for (int i = tid; i < L.units; i += NT) {
-        uint32_t t = 0;
+    // units that hold tokens of the bracket, and these
+    uint32_t nsure = finite;
+    int nlist = 0, n = 0;  // n: kept tokens of the list
+    const u64 *list = S.list;
+    if (!rules.whole) {
 #pragma unroll
-        for (int j = 0; j < UNIT / PIECE; ++j) t = max(t, tops[i * (UNIT / PIECE) + j]);
-        S.unit[i] = 0;
-        if (possible(t)) S.todo[atomicAdd(&S.ntodo, 1u)] = (uint16_t)i;
-    }
-    __syncthreads();
-    const int ntodo = (int)S.ntodo;
-    for (int q = wave; q < ntodo; q += NW) {
-        const int unit = S.todo[q], e = unit * UNIT + lane * 4;
-        const f32x4 z = load4<DT>(row, e, P.V);
-        u64 m = 0;
-        uint32_t n = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t key = key_of(z[j]);
-            const bool in = key >= kLowest && possible(key), is_sure = in && sure(key);
-            if (is_sure) {
-                const double w = W.exact(key);
-                if (w >= (double)rules.m) {
-                    m += W.to_fixed(w);
-                    ++n;
-                }
-            }
-            const u64 vote = __ballot(in && !is_sure);
-            if (vote) {
-                uint32_t base = 0;
-                if (lane == 0) base = atomicAdd(&S.nlist, (uint32_t)__popcll(vote));
-                base = __shfl((int)base, 0) + __popcll(vote & ((1ull << lane) - 1));
-                if (in && !is_sure && base < MAXLIST) S.list[base] = (u64)key << 32 | (uint32_t)~(e + j);
-            }
+        for (int i = 0; i < MOST; ++i) {
+            if (i * NT >= L.units) break;
+            const int unit = tid + i * NT;
+            const uint32_t t = max(max(tops[i][0], tops[i][1]), max(tops[i][2], tops[i][3]));
+            const bool in = unit < L.units && t >= low;
+            const u64 vote = __ballot(in);
+            uint32_t base = 0;
+            if (vote && lane == 0) base = atomicAdd(&S.ntodo, (uint32_t)__popcll(vote));
+            base = (uint32_t)__builtin_amdgcn_readfirstlane((int)base) + __popcll(vote & ((1ull << lane) - 1));
+            if (in) S.todo[base] = (uint16_t)unit;
         }
-        if (__ballot(n > 0)) {
-#pragma unroll
-            for (int o = 32; o > 0; o >>= 1) {
-                m += (u64)__shfl_xor((long long)m, o);
-                n += (uint32_t)__shfl_xor((int)n, o);
-            }
-            if (lane == 0) {
-                S.unit[unit] = m;
-                atomicAdd(&S.sure_mass, m);
-                atomicAdd(&S.nsure, n);
-            }
-        }
-    }
-    __syncthreads();
-    const int nlist = (int)S.nlist;
-    if (nlist > MAXLIST || (rules.k && nlist < k) || (bins && !nlist)) return search();
-    const u64 sure_mass = S.sure_mass;
-    int n = 0;  // kept tokens of the list
-    if (nlist) {
-        int size = 128;
-        while (size < nlist) size <<= 1;
-        for (int i = nlist + tid; i < size; i += NT) S.list[i] = 0;
         __syncthreads();
-        sort_list(S.list, size);
-        const int each = (size + NT - 1) / NT;
-        const int limit = rules.k ? k : nlist;
-        u64 m = 0;
-        for (int i = tid * each; i < min((tid + 1) * each, limit); ++i) m += W.fixed((uint32_t)(S.list[i] >> 32));
-        const u64 own = m;
-        uint32_t none = 0;
-        block_scan(S, none, m);
-        if (rules.k && rules.p < 1.f) total = block_sum(S, own);
+        const int ntodo = (int)S.ntodo;
+        nsure = 0;
+        constexpr int AHEAD = 8;  // units in flight per wave
+        for (int q0 = wave; q0 < ntodo; q0 += NW * AHEAD) {
+            int unit[AHEAD];
+            f32x4 z[AHEAD];
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                unit[i] = q0 + i * NW < ntodo ? S.todo[q0 + i * NW] : -1;
+                z[i] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                if (unit[i] >= 0) z[i] = load4<DT>(row, unit[i] * UNIT + lane * 4, P.V);
+            }
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                if (unit[i] < 0) break;
+                const int e = unit[i] * UNIT + lane * 4;
+                u64 votes[4];
+                uint32_t listed = 0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t key = key_of(z[i][j]);
+                    nsure += (uint32_t)__popcll(__ballot(key >= high));
+                    votes[j] = __ballot(key >= low && key < high);
+                    listed += (uint32_t)__popcll(votes[j]);
+                }
+                if (!listed) continue;
+                uint32_t base = 0;
+                if (lane == 0) base = atomicAdd(&S.nlist, listed);
+                base = (uint32_t)__builtin_amdgcn_readfirstlane((int)base);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t at = base + __popcll(votes[j] & ((1ull << lane) - 1));
+                    if ((votes[j] >> lane & 1) && at < MAXLIST)
+                        S.list[at] = (u64)key_of(z[i][j]) << 32 | (uint32_t)~(e + j);
+                    base += (uint32_t)__popcll(votes[j]);
+                }
+            }
+        }
+        nsure = (uint32_t)scan.sum(lane == 0 ? nsure : 0);
+        nlist = (int)S.nlist;
+        if (nlist > MAXLIST || (rules.k && nlist < k)) return search();
+        if (nlist == 0 && rules.p < 1.f && !bounded) return search();
+    }
+    if (nlist) {
+        list = sort_list(S.list, nlist);
+        const int limit = rules.k ? k : nlist, each = (limit + NT - 1) / NT;
+        u64 own = 0, sum;
+        for (int i = tid * each; i < min((tid + 1) * each, limit); ++i) own += W.fixed((uint32_t)(list[i] >> 32));
+        u64 m = scan(own, sum);
         n = limit;
         if (rules.p < 1.f) {
-            u64 goal = (u64)ceil((double)rules.p * (double)total);
-            goal = goal < 1 ? 1 : goal > total ? total : goal;
-            if (tid == 0) S.pick = 0xffffffffu;
-            __syncthreads();
-            m += sure_mass;
-            if (m < goal && m + own >= goal)
-                for (int i = tid * each; i < min((tid + 1) * each, limit); ++i) {
-                    m += W.fixed((uint32_t)(S.list[i] >> 32));
-                    if (m >= goal) {
-                        S.pick = i + 1;
-                        break;
+            if (rules.k) {
+                goal = (u64)ceil((double)rules.p * (double)sum);
+                goal = goal < 1 ? 1 : goal > sum ? sum : goal;
+            }
+            if (sure_mass + sum >= goal) {
+                if (sure_mass >= goal) return search();
+                m += sure_mass;
+                if (m < goal && m + own >= goal)
+                    for (int i = tid * each; i < min((tid + 1) * each, limit); ++i) {
+                        m += W.fixed((uint32_t)(list[i] >> 32));
+                        if (m >= goal) {
+                            S.pick = i + 1;
+                            break;
+                        }
                     }
-                }
-            __syncthreads();
-            if (S.pick == 0xffffffffu) {
-                if (sure_mass < goal) return search();
-                n = 0;
-            } else {
+                __syncthreads();
                 n = (int)S.pick;
+            } else if (!bounded) {
+                return search();
             }
         }
         if (rules.m > 0.f) {
-            uint32_t c = 0;
+            u64 c = 0;
             for (int i = tid * each; i < min((tid + 1) * each, n); ++i)
-                c += W.exact((uint32_t)(S.list[i] >> 32)) >= (double)rules.m;
-            n = (int)block_sum(S, c);
+                c += W.exact((uint32_t)(list[i] >> 32)) >= (double)rules.m;
+            n = (int)scan.sum(c);
         }
         for (int i = tid; i < n; i += NT) {
-            const u64 x = S.list[i];
-            atomicAdd(&S.unit[(uint32_t)~x / UNIT], W.fixed((uint32_t)(x >> 32)));
+            const u64 x = list[i];
+            atomicAdd(&S.kept[(uint32_t)~x / (uint32_t)L.slice], W.fixed((uint32_t)(x >> 32)));
         }
-        __syncthreads();
     }
-    const Cut cut = n ? Cut{(uint32_t)(S.list[n - 1] >> 32), (uint32_t)~S.list[n - 1]} : Cut{0xffffffffu, 0u};
-    // the unit where the running weight exceeds the target, then the token in it
-    const int each = (L.units + NT - 1) / NT;
-    u64 m = 0;
-    for (int i = tid * each; i < min((tid + 1) * each, L.units); ++i) m += S.unit[i];
-    const u64 own = m;
-    uint32_t none = 0;
-    const u64 all = block_sum(S, own);
-    const u64 target = (u64)((double)rules.u * (double)all);  // exceeds: > floor
-    block_scan(S, none, m);
-    if (m <= target && m + own > target)
-        for (int i = tid * each;; ++i) {
-            if (m + S.unit[i] > target) {
-                S.pick = i;
-                S.at = m;
-                break;
-            }
-            m += S.unit[i];
-        }
     __syncthreads();
-    const double scale = W.one / (double)all;
-    if (wave == 0) {
-        const int e = (int)S.pick * UNIT + lane * 4;
-        const f32x4 z = load4<DT>(row, e, P.V);
-        u64 w[4], run = 0;
+    const Cut cut = n ? Cut{(uint32_t)(list[n - 1] >> 32), (uint32_t)~list[n - 1]} : Cut{0xffffffffu, 0u};
+    // the slice where the running weight exceeds the target
+    u64 own = 0, all;
+#pragma unroll
+    for (int i = 0; i < SPT; ++i)
+        if (tid * SPT + i < L.slices) own += S.kept[tid * SPT + i];
+    u64 m = scan(own, all);
+    u64 target = (u64)((double)rules.u * (double)all);  // exceeds: > floor
+    if (m <= target && m + own > target) {
+#pragma unroll
+        for (int i = 0; i < SPT; ++i) {
+            const u64 x = S.kept[tid * SPT + i];
+            if (m <= target && m + x > target) {
+                S.pick = tid * SPT + i;
+                S.at = m;
+            }
+            m += x;
+        }
+    }
+    __syncthreads();
+    // the unit in it, then the token
+    const int e0 = (int)S.pick * L.slice, units = L.slice / UNIT;
+    target -= S.at;
+    auto weight = [&](uint32_t key, int e) -> u64 {  // of a kept token
+        if (key < low || !(key >= high || cut.keeps(key, e))) return 0;
+        return W.fixed(key);
+    };
+    constexpr int AHEAD = SLICE / UNIT / NW;
+    f32x4 z[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+        if (wave + i * NW < units) z[i] = load4<DT>(row, e0 + (wave + i * NW) * UNIT + lane * 4, P.V);
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+        if (wave + i * NW >= units) break;
+        const int e = e0 + (wave + i * NW) * UNIT + lane * 4;
+        u64 w = 0;
+        uint32_t last = 0;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const uint32_t key = key_of(z[j]);
-            w[j] = 0;
-            if (key >= kLowest && possible(key)) {
-                const double x = W.exact(key);
-                if (x >= (double)rules.m && (sure(key) || cut.keeps(key, e + j))) w[j] = W.to_fixed(x);
-            }
-            run += w[j];
+            const uint32_t key = key_of(z[i][j]);
+            w += weight(key, e + j);
+            if (key >= kLowest && key >= low && (key >= high || cut.keeps(key, e + j))) last = e + j + 1;
         }
-        const u64 own4 = run;
+        w = wave_sum(w);
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const u64 x = shfl_up64(run, o);
-            if (lane >= o) run += x;
-        }
-        run += S.at;
-        const u64 over = __ballot(run > target);
-        if (lane == __ffsll((long long)over) - 1) {
-            run -= own4;
-            int token = -1;
-            float logit = 0.f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                run += w[j];
-                if (token < 0 && run > target) {
-                    token = e + j;
-                    logit = z[j];
-                }
-            }
-            P.tokens[r] = token;
-            if (P.logprob) P.logprob[r] = log_of(W, key_of(logit), all);
-            if (P.kept) P.kept[r] = (int32_t)(S.nsure + n);
+        for (int o = 1; o < 64; o <<= 1) last = max(last, (uint32_t)__shfl_xor((int)last, o));
+        if (lane == 0) {
+            S.unit[wave + i * NW] = w;
+            S.last[wave + i * NW] = last;
         }
     }
+    __syncthreads();
+    if (wave == 0) {
+        const u64 w = lane < units ? S.unit[lane] : 0, run = wave_scan(w), whole = last_lane(run);
+        // a slice's weight was rounded apart from its tokens': the target may lie above them all
+        if (whole && target >= whole) target = whole - 1;
+        const u64 over = __ballot(run > target);
+        int token = -1;
+        float logit = 0.f;
+        if (over) {
+            const int u = __ffsll((long long)over) - 1;
+            target -= u ? (u64)__shfl((long long)run, u - 1) : 0;
+            const int e = e0 + u * UNIT + lane * 4;
+            const f32x4 x = load4<DT>(row, e, P.V);
+            u64 v[4], mine = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                v[j] = weight(key_of(x[j]), e + j);
+                mine += v[j];
+            }
+            u64 at = wave_scan(mine);
+            const u64 here = __ballot(at > target);
+            if (lane == __ffsll((long long)here) - 1) {
+                at -= mine;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    at += v[j];
+                    if (token < 0 && at > target) {
+                        token = e + j;
+                        logit = x[j];
+                    }
+                }
+            }
+        } else if (lane == 0) {  // tokens too light to count one by one: the last of them
+            uint32_t last = 1;
+            for (int u = 0; u < units; ++u) last = max(last, S.last[u]);
+            token = (int)last - 1;
+            logit = load<DT>(row, token);
+        }
+        if (token >= 0) {
+            P.tokens[r] = token;
+            if (P.logprob) P.logprob[r] = log_of(W, key_of(logit), all);
+            if (P.kept) P.kept[r] = (int32_t)(nsure + n);
+        }
+    }
+    const double scale = W.one / (double)all;
+    if (tid == 0) L.spread[r] = Spread{scale, top, high};
     if (!P.probs) return;
     float *probs = P.probs + (size_t)r * P.V;
     for (int i = tid; i < n; i += NT) {
-        const u64 x = S.list[i];
+        const u64 x = list[i];
         probs[(uint32_t)~x] = (float)(W.exact((uint32_t)(x >> 32)) * scale);
-    }
-    if (S.nsure == 0) return;
-    for (int q = wave; q < ntodo; q += NW) {
-        const int e = S.todo[q] * UNIT + lane * 4;
-        const f32x4 z = load4<DT>(row, e, P.V);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t key = key_of(z[j]);
-            if (key < kLowest || !possible(key) || !sure(key)) continue;
-            const double w = W.exact(key);
-            if (w >= (double)rules.m) probs[e + j] = (float)(w * scale);
-        }
     }
 }
 
@@ -1029,60 +1139,40 @@ __global__ __launch_bounds__(NT) void pick_kernel(SampleProblem P, Scan L, int s
     pick_row<DT>(P, L, blockIdx.x, shift, idbits, S);
 }
 
-// The dense probabilities of the rows without rules, a slice of SLICE tokens per workgroup.
+// The probabilities of what is surely kept, a slice of SLICE tokens per workgroup (rows without rules:
+// of every token).
 template <int DT>
-__global__ __launch_bounds__(ST) void whole_kernel(SampleProblem P, Scan L, int shift) {
+__global__ __launch_bounds__(ST) void spread_kernel(SampleProblem P, Scan L) {
     __shared__ double table[64];
-    __shared__ uint32_t top_key, bad;
-    __shared__ u64 wmass[ST / 64];
     const int per = (P.V + SLICE - 1) / SLICE, r = blockIdx.x / per, s = blockIdx.x % per, tid = threadIdx.x;
+    const Spread spread = L.spread[r];
     const Rules rules(P, r);
-    if (!rules.whole) return;
+    if (!rules.whole && spread.least > spread.top) return;
     const char *row = row_of<DT>(P, r);
     f32x4 z[SLICE / ST / 4];
 #pragma unroll
     for (int i = 0; i < SLICE / ST / 4; ++i) z[i] = load4<DT>(row, s * SLICE + (i * ST + tid) * 4, P.V);
     fill_table(table);
-    if (tid == 0) top_key = bad = 0;
     __syncthreads();
-    const SliceStat *stat = L.stat + (size_t)r * L.slices;
-    uint32_t top = 0, b = 0;
-    for (int i = tid; i < L.slices; i += ST) {
-        top = max(top, stat[i].top);
-        b |= stat[i].bad;
-    }
-    atomicMax(&top_key, top);
-    if (b) atomicOr(&bad, 1u);
-    __syncthreads();
-    const Weights W{(double)logit_of(top_key), 1.0 / (double)rules.T, (double)(1ull << shift), table};
-    const bool ok = !bad && top_key >= kLowest;
-    u64 total = 0;
-    for (int i = tid; i < L.slices; i += ST)
-        if (ok && stat[i].finite) total += W.to_fixed(stat[i].mass * W.exact(stat[i].top));
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) total += (u64)__shfl_xor((long long)total, o);
-    if (tid % 64 == 0) wmass[tid / 64] = total;
-    __syncthreads();
-    total = 0;
-#pragma unroll
-    for (int w = 0; w < ST / 64; ++w) total += wmass[w];
-    const double scale = ok ? W.one / (double)total : 0.0;
+    const Weights W{(double)logit_of(spread.top), 1.0 / (double)rules.T, 1.0, table};
     float *probs = P.probs + (size_t)r * P.V;
 #pragma unroll
     for (int i = 0; i < SLICE / ST / 4; ++i) {
         const int e = s * SLICE + (i * ST + tid) * 4;
         f32x4 q;
+        bool in[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const uint32_t key = key_of(z[i][j]);
-            q[j] = ok && key >= kLowest ? (float)(W.exact(key) * scale) : 0.f;
+            in[j] = key >= spread.least;
+            q[j] = in[j] ? (float)(W.exact(key) * spread.scale) : 0.f;
         }
-        if (e + 3 < P.V) {
+        if (rules.whole && e + 3 < P.V) {
             __builtin_nontemporal_store(q, reinterpret_cast<f32x4_any *>(probs + e));
         } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                if (e + j < P.V) probs[e + j] = q[j];
+                if (e + j < P.V && (rules.whole || in[j])) probs[e + j] = q[j];
         }
     }
 }
@@ -1110,7 +1200,8 @@ Scan layout(const SampleProblem &p, char *ws, size_t &bytes) {
     const size_t R = (size_t)p.R;
     L.stat = (SliceStat *)take(R * L.slices * sizeof(SliceStat));
     L.tops = (uint32_t *)take(R * L.pieces * 4);
-    L.hist = (float *)take(R * L.slices * HB * 4);
+    L.hist = (u64 *)take(R * L.slices * HB * sizeof(u64));
+    L.spread = (Spread *)take(R * sizeof(Spread));
     bytes = off ? off : 256;
     return L;
 }
@@ -1133,8 +1224,8 @@ hipError_t launch(const SampleProblem &p, char *ws, hipStream_t st) {
         hipLaunchKernelGGL((scan_kernel<DT, 2048 / ST>), scan, dim3(ST), 0, st, p, L);
     hipLaunchKernelGGL((pick_kernel<DT>), dim3((unsigned)p.R), dim3(NT), 0, st, p, L, shift, idbits);
     if (p.probs) {
-        const dim3 whole((unsigned)(p.R * ((p.V + SLICE - 1) / SLICE)));
-        hipLaunchKernelGGL((whole_kernel<DT>), whole, dim3(ST), 0, st, p, L, shift);
+        const dim3 spread((unsigned)(p.R * ((p.V + SLICE - 1) / SLICE)));
+        hipLaunchKernelGGL((spread_kernel<DT>), spread, dim3(ST), 0, st, p, L);
     }
     return hipGetLastError();
 }

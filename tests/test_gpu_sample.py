@@ -102,6 +102,27 @@ def test_one_rule_alone(name, value, dtype):
         Call(logits(len(value), V, 3), uniforms(len(value), 4), dtype, **{name: value}).run().check()
 
 
+@pytest.mark.parametrize("T", [1e-20, 1e-3, 50.0, 1e6, 1e30])
+def test_top_p_and_min_p_at_extreme_temperatures(T):
+    """Weights that all but vanish beside the largest, or all but equal it."""
+    for V in (3001, 40000):
+        R = 8
+        p, m = np.array([0.3, 0.9, 1, 1] * 2, np.float32), np.array([0, 0, 0.2, 0.99999] * 2, np.float32)
+        z = logits(R, V, 5, 2.0)
+        z[4:] *= 1e-30
+        Call(z, uniforms(R, 3), temperature=np.full(R, T, np.float32), top_p=p, min_p=m).run().check()
+
+
+@pytest.mark.parametrize("V", [9000, 128256])
+def test_top_p_with_min_p_and_deep_rows(V):
+    """Where one of the two rules cuts far above the other, and nuclei of many tokens."""
+    R = 24
+    p = np.array([0.2, 0.6, 0.9, 0.99, 0.9999, 1.0] * 4, np.float32)
+    m = np.repeat(np.array([1e-9, 1e-4, 0.02, 0.7], np.float32), 6)
+    Call(logits(R, V, 6, 2.5), uniforms(R, 7), top_p=p, min_p=m).run().check()
+    Call(logits(R, V, 6, 1.0), uniforms(R, 7), "bf16", top_p=p).run().check()
+
+
 @pytest.mark.parametrize("V", [3001, 40000])
 @pytest.mark.parametrize("spread", [0.0, 0.01, 0.3, 1.0])
 def test_flat_rows(V, spread):
