@@ -50,36 +50,41 @@ __device__ __forceinline__ float load(const void *row, int i) {
     return ((const float *)row)[i];
 }
 
-// exp(x), x <= 0, in 64 bits: x = (64 k + j) ln 2 / 64 + r, exp(x) = 2^k 2^(j/64) exp(r) with the 64
-// powers in a table and a polynomial of degree 5 for |r| <= ln 2 / 128 (Tang's table-driven
-// method; the terms left out are 4e-17).  ln 2 / 64 = kLnHi + kLnLo, kLnHi with 32 bits, so that
-// its product with k is exact.
-constexpr double kLnHi = 0x1.62e42fee00000p-7, kLnLo = 0x1.a39ef35793c76p-39, kPerLn = 0x1.71547652b82fep+6;
+// 2^(y / 128), y <= 0, in 64 bits: y = 128 k + j + f, 2^k 2^(j/128) 2^(f/128) with the 128 powers in a
+// table and a polynomial of degree 4 for |f| <= 1/2 (the table-driven method of Tang; the terms
+// left out are 1e-15).
+constexpr int POWERS = 1 << 7;
+constexpr double kLn = 0.693147180559945309417 / POWERS;
 
-__device__ __forceinline__ void fill_table(double *table) {  // by the first 64 threads
-    if (threadIdx.x < 64) table[threadIdx.x] = exp2((double)threadIdx.x / 64.0);
+__device__ __forceinline__ void fill_table(double *table) {  // by the first POWERS threads
+    if (threadIdx.x < POWERS) table[threadIdx.x] = exp2((double)threadIdx.x / POWERS);
 }
-__device__ __forceinline__ double exp_of(double x, const double *table) {
-    x = fmax(x, -800.0);
-    const double q = rint(x * kPerLn), r = fma(-q, kLnLo, fma(-q, kLnHi, x));
+__device__ __forceinline__ double power_of(double y, const double *table) {
+    y = fmax(y, -160000.0);  // (2^-1250 is 0)
+    const double q = rint(y), f = y - q;
     const int k = (int)q;
-    double e = fma(r, 1.0 / 120, 1.0 / 24);
-    e = fma(r, e, 1.0 / 6);
-    e = fma(r, e, 0.5);
-    e = fma(r, e, 1.0);
-    const double t = table[k & 63];
-    return ldexp(fma(t * r, e, t), k >> 6);
+    double e = fma(f, kLn * kLn * kLn * kLn / 24, kLn * kLn * kLn / 6);
+    e = fma(f, e, kLn * kLn / 2);
+    e = fma(f, e, kLn);
+    const double t = table[k & (POWERS - 1)];
+    return ldexp(fma(t * f, e, t), k >> 7);
 }
 
-// Weights of a row relative to its largest logit, in 64 bits and as fixed-point numbers.
+// Weights of a row relative to its largest logit, in 64 bits and as fixed-point numbers of at most
+// 2^50.
 struct Weights {
-    double top, inv_T, one;  // one: 2^shift, the fixed-point weight of the largest logit
+    double top, per, one;  // per: 128 / (T ln 2); one: the fixed-point weight of the largest logit
     const double *table;
+    __device__ __forceinline__ Weights(uint32_t top_key, float T, int shift, const double *table_)
+        : top((double)logit_of(top_key)), per(1.0 / kLn / (double)T), one((double)(1ull << shift)), table(table_) {}
     __device__ __forceinline__ double exact(uint32_t key) const {
-        return exp_of(((double)logit_of(key) - top) * inv_T, table);
+        return power_of(((double)logit_of(key) - top) * per, table);
     }
-    __device__ __forceinline__ u64 to_fixed(double w) const { return (u64)rint(w * one); }
+    __device__ __forceinline__ u64 to_fixed(double w) const {  // w <= 1: rounded by the sum with 2^52
+        return (u64)__double_as_longlong(fma(w, one, 0x1p52)) - 0x4330000000000000ull;
+    }
     __device__ __forceinline__ u64 fixed(uint32_t key) const { return to_fixed(exact(key)); }
+    __device__ __forceinline__ double log_weight(uint32_t key) const { return ((double)logit_of(key) - top) * per * kLn; }
 };
 
 // A row's rules; one that is outside its range leaves the row without a target.
@@ -215,7 +220,7 @@ __device__ __forceinline__ void clear_bins(Shared &S) {
 // The element of the order where the running count (or mass) reaches `target`, which the
 // row's finite logits do reach; `kept` gets the mass up to and with it.
 template <bool MASS, class ForEach>
-__device__ Cut search(Shared &S, const ForEach &each, const Weights &W, u64 target, int idbits, u64 &kept) {
+__device__ __forceinline__ Cut search(Shared &S, const ForEach &each, const Weights &W, u64 target, int idbits, u64 &kept) {
     uint32_t prefix = 0, above_c = 0;
     u64 above_m = 0;
     const int shifts[3] = {32 - BITS, 32 - 2 * BITS, 0};
@@ -272,7 +277,7 @@ struct SearchLds {
 };
 
 template <int DT>
-__device__ void search_row(const SampleProblem &P, int r, const Rules &rules, int shift, int idbits, SearchLds &lds,
+__device__ __forceinline__ void search_row(const SampleProblem &P, int r, const Rules &rules, int shift, int idbits, SearchLds &lds,
                            const double *table) {
     Shared &S = lds.s;
     u64 *csum = lds.csum;
@@ -304,7 +309,7 @@ __device__ void search_row(const SampleProblem &P, int r, const Rules &rules, in
         if (tid == 0) no_token(P, r);
         return;
     }
-    const Weights W{(double)logit_of(top), 1.0 / (double)rules.T, (double)(1ull << shift), table};
+    const Weights W(top, rules.T, shift, table);
 
     auto each = [&](auto f) {
         for (int i = tid; i < P.V; i += NT) f((uint32_t)i, key_of(load<DT>(row, i)));
@@ -343,7 +348,7 @@ __device__ void search_row(const SampleProblem &P, int r, const Rules &rules, in
         for (int i = c * chunk + lane; i < end; i += 64) {
             double w;
             if (kept(i, key_of(load<DT>(row, i)), w)) {
-                m += (u64)rint(w * W.one);
+                m += W.to_fixed(w);
                 ++n;
             }
         }
@@ -381,7 +386,7 @@ __device__ void search_row(const SampleProblem &P, int r, const Rules &rules, in
             const int i = i0 + lane;
             double w = 0;
             const uint32_t key = i < end ? key_of(load<DT>(row, i)) : 0;
-            const u64 mine = kept(i, key, w) ? (u64)rint(w * W.one) : 0;
+            const u64 mine = kept(i, key, w) ? W.to_fixed(w) : 0;
             u64 run = mine;
 #pragma unroll
             for (int o = 1; o < 64; o <<= 1) {
@@ -395,7 +400,7 @@ __device__ void search_row(const SampleProblem &P, int r, const Rules &rules, in
                     P.tokens[r] = i;
                     if (P.logprob)
                         P.logprob[r] =
-                            (float)(((double)logit_of(key) - W.top) * W.inv_T - log((double)total / W.one));
+                            (float)(W.log_weight(key) - log((double)total / W.one));
                 }
                 break;
             }
@@ -415,7 +420,7 @@ __device__ void search_row(const SampleProblem &P, int r, const Rules &rules, in
 template <int DT>
 __global__ __launch_bounds__(NT) void search_kernel(SampleProblem P, int shift, int idbits) {
     __shared__ SearchLds lds;
-    __shared__ double table[64];
+    __shared__ double table[POWERS];
     fill_table(table);
     search_row<DT>(P, blockIdx.x, Rules(P, blockIdx.x), shift, idbits, lds, table);
 }
@@ -424,7 +429,9 @@ __global__ __launch_bounds__(NT) void search_kernel(SampleProblem P, int shift, 
 // The two launches.
 
 constexpr int ST = 256;         // threads of a slice's workgroup
-constexpr int PIECE = 64;       // logits per recorded maximum
+constexpr int PIECE = 64;       // logits per recorded maximum,
+constexpr int SHORT = 4;        // or in vocabularies of up to SHORTV (so that a bracket by top-k stays narrow)
+constexpr int SHORTV = 65536;
 constexpr int UNIT = 256;       // logits read again together
 constexpr int HB = 256;         // histogram bins, 1/16 of a temperature wide, below the slice's largest logit
 constexpr int SLICE = 8192;     // logits per slice (of a dense row's second pass, too)
@@ -448,7 +455,7 @@ struct Spread {
 };
 
 struct Scan {
-    int slice, slices, pieces, units;  // logits per slice; slices, pieces and units of a row
+    int slice, slices, piece, pieces, units;  // logits per slice and piece; slices, pieces and units of a row
     SliceStat *stat;                   // [R][slices]
     uint32_t *tops;                    // [R][pieces]: key of each piece's largest logit
     u64 *hist;                         // [R][slices][HB]: weights at 2^kHistShift, the last bin: the rest
@@ -514,7 +521,7 @@ __device__ __forceinline__ u64 wave_sum(u64 x) { return last_lane(wave_scan(x));
 // One slice: EPT logits per thread, held in registers between the maximum and the weights.
 template <int DT, int EPT>
 __global__ __launch_bounds__(ST) void scan_kernel(SampleProblem P, Scan L) {
-    __shared__ double table[64];
+    __shared__ double table[POWERS];
     __shared__ u64 hist[HB], wmass[ST / 64];
     __shared__ uint32_t wtop[ST / 64], wbad[ST / 64], wfinite[ST / 64];
     const int s = blockIdx.x % L.slices, r = blockIdx.x / L.slices;
@@ -554,9 +561,14 @@ __global__ __launch_bounds__(ST) void scan_kernel(SampleProblem P, Scan L) {
             t = max(t, key);
             finite += key >= kLowest;
         }
+        const int e = at + i * ST * 4;
+        if (L.piece == PIECE) {
 #pragma unroll
-        for (int o = 1; o < PIECE / 4; o <<= 1) t = max(t, (uint32_t)__shfl_xor((int)t, o));
-        if (lane % (PIECE / 4) == 0) tops[(at + i * ST * 4) / PIECE] = t;
+            for (int o = 1; o < PIECE / 4; o <<= 1) t = max(t, (uint32_t)__shfl_xor((int)t, o));
+            if (lane % (PIECE / 4) == 0 && e < L.units * UNIT) tops[e / PIECE] = t;
+        } else if (e < L.units * UNIT) {
+            tops[e / SHORT] = t;
+        }
         top = max(top, t);
     }
 #pragma unroll
@@ -580,7 +592,7 @@ __global__ __launch_bounds__(ST) void scan_kernel(SampleProblem P, Scan L) {
     }
     SliceStat st{top, bad, finite, 0, 0};
     if (weighs && finite && !bad) {
-        const Weights W{(double)logit_of(top), 1.0 / (double)rules.T, (double)(1ull << kHistShift), table};
+        const Weights W(top, rules.T, kHistShift, table);
         u64 m = 0;
         const float per = 16.f / rules.T, first = bin_of(logit_of(top), per);
 #pragma unroll
@@ -605,7 +617,7 @@ __global__ __launch_bounds__(ST) void scan_kernel(SampleProblem P, Scan L) {
 
 // What a row's workgroup keeps in LDS.
 struct PickLds {
-    double table[64];
+    double table[POWERS];
     union {
         u64 list[MAXLIST + MAXCOUNTED];  // (key, ~id) of the tokens inside the bracket; the last ones: in order
         SearchLds search;                // instead: the search of the logits themselves
@@ -653,7 +665,7 @@ struct BlockScan {
 };
 
 __device__ __forceinline__ float log_of(const Weights &W, uint32_t key, u64 total) {
-    return (float)(((double)logit_of(key) - W.top) * W.inv_T - log((double)total / W.one));
+    return (float)(W.log_weight(key) - log((double)total / W.one));
 }
 
 // Descending order of n numbers of list[], into list[MAXLIST ..] (few: each by counting the larger ones)
@@ -733,9 +745,9 @@ __device__ __forceinline__ uint32_t first_key(float b, float per) {
     return lo;
 }
 
-// A row's token.
+// A row's token; false (for every thread) where the bracket fails.
 template <int DT>
-__device__ void pick_row(const SampleProblem &P, const Scan &L, int r, int shift, int idbits, PickLds &S) {
+__device__ __forceinline__ bool pick_row(const SampleProblem &P, const Scan &L, int r, int shift, PickLds &S) {
     const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
     const char *row = row_of<DT>(P, r);
     BlockScan scan{S};
@@ -747,13 +759,15 @@ __device__ void pick_row(const SampleProblem &P, const Scan &L, int r, int shift
         st[i] = SliceStat{0, 0, 0, 0, 0};
         if (tid + i * NT < L.slices) st[i] = L.stat[(size_t)r * L.slices + tid + i * NT];
     }
-    constexpr int MOST = MAXV / UNIT / NT;  // units per thread
+    constexpr int MOST = MAXV / UNIT / NT;  // groups of four pieces per thread
+    static_assert(SHORTV / (4 * SHORT) <= MOST * NT, "pieces");
+    const int groups = L.pieces / 4;
     u32x4 tops[MOST];
     const u32x4 *all_tops = reinterpret_cast<const u32x4 *>(L.tops + (size_t)r * L.pieces);
 #pragma unroll
     for (int i = 0; i < MOST; ++i) {
         tops[i] = u32x4{0, 0, 0, 0};
-        if (tid + i * NT < L.units) tops[i] = all_tops[tid + i * NT];
+        if (tid + i * NT < groups) tops[i] = all_tops[tid + i * NT];
     }
     const Rules rules(P, r);
     fill_table(S.table);
@@ -792,9 +806,9 @@ __device__ void pick_row(const SampleProblem &P, const Scan &L, int r, int shift
             L.spread[r] = spread;
             no_token(P, r);
         }
-        return;
+        return true;
     }
-    const Weights W{(double)logit_of(top), 1.0 / (double)rules.T, (double)(1ull << shift), S.table};
+    const Weights W(top, rules.T, shift, S.table);
     const float per = 16.f / rules.T, first = bin_of((float)W.top, per);
     if (rules.k == 0) {
 #pragma unroll
@@ -808,11 +822,6 @@ __device__ void pick_row(const SampleProblem &P, const Scan &L, int r, int shift
     } else {
         for (int s = tid; s < L.slices; s += NT) S.kept[s] = 0;
     }
-    auto search = [&] {
-        __syncthreads();
-        if (tid == 0) L.spread[r] = Spread{0.0, top, 0xffffffffu};
-        search_row<DT>(P, r, rules, shift, idbits, S.search, S.table);
-    };
     // The bracket: tokens with key >= high are surely kept, those with key >= low may be.
     const int k = min(rules.k, (int)finite);
     uint32_t low = kLowest, high = 0xffffffffu;
@@ -828,7 +837,7 @@ __device__ void pick_row(const SampleProblem &P, const Scan &L, int r, int shift
         for (int i = 0; i < SPT; ++i)
             if (tid + i * NT < L.slices) S.kept[tid + i * NT] = to_row(st[i].mass, tid + i * NT);
     } else if (rules.k == 0) {
-        if (!(fabsf(first) < kBinLimit)) return search();
+        if (!(fabsf(first) < kBinLimit)) return false;
         __syncthreads();
         u64 mine = 0;
 #pragma unroll
@@ -874,7 +883,7 @@ __device__ void pick_row(const SampleProblem &P, const Scan &L, int r, int shift
                 bounded = true;
             }
         }
-        if (lo_bin >= HB - 1) return search();
+        if (lo_bin >= HB - 1) return false;
         low = first_key(first - (float)lo_bin, per);
         high = first_key(first - (float)hi_bin + 1.f, per);
         if (tid == hi_bin) S.at = before;
@@ -906,7 +915,7 @@ __device__ void pick_row(const SampleProblem &P, const Scan &L, int r, int shift
             u64 counts = 0;
 #pragma unroll
             for (int i = 0; i < MOST; ++i)
-                if (i * NT < L.units) {
+                if (i * NT < groups) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -919,8 +928,7 @@ __device__ void pick_row(const SampleProblem &P, const Scan &L, int r, int shift
 #pragma unroll
             for (int w = 0; w < NW; ++w) counts += S.wave[scan.turn][w];
             scan.turn ^= 1;
-            int c = 3;
-            while (c > 0 && (int)(counts >> (21 * (c - 1)) & 0x1fffff) < k) --c;
+            const int c = ((int)(counts & 0x1fffff) >= k) + ((int)(counts >> 21 & 0x1fffff) >= k) + ((int)(counts >> 42) >= k);
             prefix |= (uint32_t)c << bit;
         }
         low = max(prefix, kLowest);
@@ -932,7 +940,7 @@ __device__ void pick_row(const SampleProblem &P, const Scan &L, int r, int shift
     if (!rules.whole) {
 #pragma unroll
         for (int i = 0; i < MOST; ++i) {
-            if (i * NT >= L.units) break;
+            if (L.piece != PIECE || i * NT >= L.units) break;
             const int unit = tid + i * NT;
             const uint32_t t = max(max(tops[i][0], tops[i][1]), max(tops[i][2], tops[i][3]));
             const bool in = unit < L.units && t >= low;
@@ -943,29 +951,35 @@ __device__ void pick_row(const SampleProblem &P, const Scan &L, int r, int shift
             if (in) S.todo[base] = (uint16_t)unit;
         }
         __syncthreads();
-        const int ntodo = (int)S.ntodo;
+        const int ntodo = L.piece == PIECE ? (int)S.ntodo : L.units;  // (a group of short pieces is no unit)
         nsure = 0;
-        constexpr int AHEAD = 8;  // units in flight per wave
-        for (int q0 = wave; q0 < ntodo; q0 += NW * AHEAD) {
+        // the bracket as logits: comparisons give the masks (nothing is >= NaN; -0 equals 0)
+        const float from = logit_of(low), to = logit_of(high);
+        constexpr int AHEAD = 8;  // units in flight per wave, twice
+        struct Batch {
             int unit[AHEAD];
             f32x4 z[AHEAD];
+        };
+        auto fetch = [&](int q0, Batch &b) {
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) {
-                unit[i] = q0 + i * NW < ntodo ? S.todo[q0 + i * NW] : -1;
-                z[i] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-                if (unit[i] >= 0) z[i] = load4<DT>(row, unit[i] * UNIT + lane * 4, P.V);
+                const int q = q0 + i * NW;
+                b.unit[i] = q >= ntodo ? -1 : L.piece == PIECE ? __builtin_amdgcn_readfirstlane((int)S.todo[q]) : q;
+                if (b.unit[i] >= 0) b.z[i] = load4<DT>(row, b.unit[i] * UNIT + lane * 4, P.V);
             }
+        };
+        auto take = [&](const Batch &b) {
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) {
-                if (unit[i] < 0) break;
-                const int e = unit[i] * UNIT + lane * 4;
+                if (b.unit[i] < 0) break;
+                const int e = b.unit[i] * UNIT + lane * 4;
                 u64 votes[4];
                 uint32_t listed = 0;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const uint32_t key = key_of(z[i][j]);
-                    nsure += (uint32_t)__popcll(__ballot(key >= high));
-                    votes[j] = __ballot(key >= low && key < high);
+                    const u64 above = __ballot(b.z[i][j] >= to);
+                    votes[j] = __ballot(b.z[i][j] >= from) & ~above;
+                    nsure += (uint32_t)__popcll(above);
                     listed += (uint32_t)__popcll(votes[j]);
                 }
                 if (!listed) continue;
@@ -976,15 +990,23 @@ __device__ void pick_row(const SampleProblem &P, const Scan &L, int r, int shift
                 for (int j = 0; j < 4; ++j) {
                     const uint32_t at = base + __popcll(votes[j] & ((1ull << lane) - 1));
                     if ((votes[j] >> lane & 1) && at < MAXLIST)
-                        S.list[at] = (u64)key_of(z[i][j]) << 32 | (uint32_t)~(e + j);
+                        S.list[at] = (u64)key_of(b.z[i][j]) << 32 | (uint32_t)~(e + j);
                     base += (uint32_t)__popcll(votes[j]);
                 }
             }
+        };
+        Batch one, two;
+        fetch(wave, one);
+        for (int q0 = wave; q0 < ntodo; q0 += 2 * NW * AHEAD) {
+            fetch(q0 + NW * AHEAD, two);
+            take(one);
+            fetch(q0 + 2 * NW * AHEAD, one);
+            take(two);
         }
         nsure = (uint32_t)scan.sum(lane == 0 ? nsure : 0);
         nlist = (int)S.nlist;
-        if (nlist > MAXLIST || (rules.k && nlist < k)) return search();
-        if (nlist == 0 && rules.p < 1.f && !bounded) return search();
+        if (nlist > MAXLIST || (rules.k && nlist < k)) return false;
+        if (nlist == 0 && rules.p < 1.f && !bounded) return false;
     }
     if (nlist) {
         list = sort_list(S.list, nlist);
@@ -999,7 +1021,7 @@ __device__ void pick_row(const SampleProblem &P, const Scan &L, int r, int shift
                 goal = goal < 1 ? 1 : goal > sum ? sum : goal;
             }
             if (sure_mass + sum >= goal) {
-                if (sure_mass >= goal) return search();
+                if (sure_mass >= goal) return false;
                 m += sure_mass;
                 if (m < goal && m + own >= goal)
                     for (int i = tid * each; i < min((tid + 1) * each, limit); ++i) {
@@ -1012,7 +1034,7 @@ __device__ void pick_row(const SampleProblem &P, const Scan &L, int r, int shift
                 __syncthreads();
                 n = (int)S.pick;
             } else if (!bounded) {
-                return search();
+                return false;
             }
         }
         if (rules.m > 0.f) {
@@ -1125,25 +1147,30 @@ __device__ void pick_row(const SampleProblem &P, const Scan &L, int r, int shift
     }
     const double scale = W.one / (double)all;
     if (tid == 0) L.spread[r] = Spread{scale, top, high};
-    if (!P.probs) return;
+    if (!P.probs) return true;
     float *probs = P.probs + (size_t)r * P.V;
     for (int i = tid; i < n; i += NT) {
         const u64 x = list[i];
         probs[(uint32_t)~x] = (float)(W.exact((uint32_t)(x >> 32)) * scale);
     }
+    return true;
 }
 
 template <int DT>
 __global__ __launch_bounds__(NT) void pick_kernel(SampleProblem P, Scan L, int shift, int idbits) {
     __shared__ PickLds S;
-    pick_row<DT>(P, L, blockIdx.x, shift, idbits, S);
+    const int r = blockIdx.x;
+    if (pick_row<DT>(P, L, r, shift, S)) return;
+    __syncthreads();
+    if (threadIdx.x == 0) L.spread[r] = Spread{0.0, 0u, 0xffffffffu};
+    search_row<DT>(P, r, Rules(P, r), shift, idbits, S.search, S.table);
 }
 
 // The probabilities of what is surely kept, a slice of SLICE tokens per workgroup (rows without rules:
 // of every token).
 template <int DT>
 __global__ __launch_bounds__(ST) void spread_kernel(SampleProblem P, Scan L) {
-    __shared__ double table[64];
+    __shared__ double table[POWERS];
     const int per = (P.V + SLICE - 1) / SLICE, r = blockIdx.x / per, s = blockIdx.x % per, tid = threadIdx.x;
     const Spread spread = L.spread[r];
     const Rules rules(P, r);
@@ -1154,7 +1181,7 @@ __global__ __launch_bounds__(ST) void spread_kernel(SampleProblem P, Scan L) {
     for (int i = 0; i < SLICE / ST / 4; ++i) z[i] = load4<DT>(row, s * SLICE + (i * ST + tid) * 4, P.V);
     fill_table(table);
     __syncthreads();
-    const Weights W{(double)logit_of(spread.top), 1.0 / (double)rules.T, 1.0, table};
+    const Weights W(spread.top, rules.T, 0, table);
     float *probs = P.probs + (size_t)r * P.V;
 #pragma unroll
     for (int i = 0; i < SLICE / ST / 4; ++i) {
@@ -1189,8 +1216,9 @@ Scan layout(const SampleProblem &p, char *ws, size_t &bytes) {
     const int large = (p.V + SLICE - 1) / SLICE;
     L.slice = (long long)p.R * large < 2 * kCus && p.V <= 2048 * MAXSLICES ? 2048 : SLICE;
     L.slices = (p.V + L.slice - 1) / L.slice;
-    L.pieces = L.slices * L.slice / PIECE;
-    L.units = L.slices * L.slice / UNIT;
+    L.units = (p.V + UNIT - 1) / UNIT;
+    L.piece = L.units * UNIT <= SHORTV ? SHORT : PIECE;
+    L.pieces = L.units * UNIT / L.piece;
     size_t off = 0;
     auto take = [&](size_t n) {
         char *at = ws ? ws + off : nullptr;
