@@ -437,6 +437,7 @@ constexpr int HB = 256;         // histogram bins, 1/16 of a temperature wide, b
 constexpr int SLICE = 8192;     // logits per slice (of a dense row's second pass, too)
 constexpr int MAXV = 1 << 20;   // largest vocabulary of this path
 constexpr int MAXLIST = 4096;   // tokens inside a row's bracket
+constexpr int MAXTODO = 4096;   // pieces that may hold one, by number (more: every piece of the row)
 constexpr int MAXCOUNTED = 512;  // up to so many are put in order by counting
 constexpr int kHistShift = 50;  // 8,192 weights of a slice stay below 2^63
 constexpr int MAXSLICES = MAXV / SLICE > 512 ? MAXV / SLICE : 512;
@@ -455,9 +456,9 @@ struct Spread {
 };
 
 struct Scan {
-    int slice, slices, piece, pieces, units;  // logits per slice and piece; slices, pieces and units of a row
+    int slice, slices, piece, pieces;  // logits per slice and piece; slices and pieces of a row
     SliceStat *stat;                   // [R][slices]
-    uint32_t *tops;                    // [R][pieces]: key of each piece's largest logit
+    uint16_t *tops;                    // [R][pieces]: upper half of the key of each piece's largest logit
     u64 *hist;                         // [R][slices][HB]: weights at 2^kHistShift, the last bin: the rest
     Spread *spread;                    // [R]
 };
@@ -467,22 +468,25 @@ typedef f32x4 f32x4_any __attribute__((aligned(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef u32x2 u32x2_any __attribute__((aligned(2)));
 
-// Four logits from i on; -inf past the vocabulary.
+// Four logits from i on; -inf past the vocabulary (of at least four: where they would pass its end, the
+// last four are loaded and moved).
 template <int DT>
 __device__ __forceinline__ f32x4 load4(const void *row, int i, int V) {
-    f32x4 z = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-    if (i + 3 < V) {
-        if constexpr (DT == kBF16) {
-            const u32x2 x = *reinterpret_cast<const u32x2_any *>((const uint16_t *)row + i);
-            z = f32x4{__uint_as_float(x[0] << 16), __uint_as_float(x[0] & 0xffff0000u), __uint_as_float(x[1] << 16),
-                      __uint_as_float(x[1] & 0xffff0000u)};
-        } else {
-            z = *reinterpret_cast<const f32x4_any *>((const float *)row + i);
-        }
+    const int at = min(i, V - 4), d = i - at;
+    f32x4 z;
+    if constexpr (DT == kBF16) {
+        const u32x2 x = *reinterpret_cast<const u32x2_any *>((const uint16_t *)row + at);
+        z = f32x4{__uint_as_float(x[0] << 16), __uint_as_float(x[0] & 0xffff0000u), __uint_as_float(x[1] << 16),
+                  __uint_as_float(x[1] & 0xffff0000u)};
     } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (i + j < V) z[j] = load<DT>(row, i + j);
+        z = *reinterpret_cast<const f32x4_any *>((const float *)row + at);
+    }
+    if (d) {
+        const float none = -INFINITY, z1 = z[1], z2 = z[2], z3 = z[3];
+        z[0] = d == 1 ? z1 : d == 2 ? z2 : d == 3 ? z3 : none;
+        z[1] = d == 1 ? z2 : d == 2 ? z3 : none;
+        z[2] = d == 1 ? z3 : none;
+        z[3] = none;
     }
     return z;
 }
@@ -550,7 +554,7 @@ __global__ __launch_bounds__(ST) void scan_kernel(SampleProblem P, Scan L) {
         hist[tid] = 0;
     }
     uint32_t top = 0, bad = 0, finite = 0;
-    uint32_t *tops = L.tops + (size_t)r * L.pieces;
+    uint16_t *tops = L.tops + (size_t)r * L.pieces;
 #pragma unroll
     for (int i = 0; i < EPT / 4; ++i) {
         uint32_t t = 0;
@@ -565,9 +569,9 @@ __global__ __launch_bounds__(ST) void scan_kernel(SampleProblem P, Scan L) {
         if (L.piece == PIECE) {
 #pragma unroll
             for (int o = 1; o < PIECE / 4; o <<= 1) t = max(t, (uint32_t)__shfl_xor((int)t, o));
-            if (lane % (PIECE / 4) == 0 && e < L.units * UNIT) tops[e / PIECE] = t;
-        } else if (e < L.units * UNIT) {
-            tops[e / SHORT] = t;
+            if (lane % (PIECE / 4) == 0 && e < L.pieces * PIECE) tops[e / PIECE] = (uint16_t)(t >> 16);
+        } else if (e < L.pieces * SHORT) {
+            tops[e / SHORT] = (uint16_t)(t >> 16);
         }
         top = max(top, t);
     }
@@ -622,7 +626,7 @@ struct PickLds {
         u64 list[MAXLIST + MAXCOUNTED];  // (key, ~id) of the tokens inside the bracket; the last ones: in order
         SearchLds search;                // instead: the search of the logits themselves
     };
-    uint16_t todo[MAXV / UNIT];  // units that may hold tokens of the bracket
+    uint16_t todo[MAXTODO];      // pieces that may hold tokens of the bracket
     double scale[MAXSLICES];     // a slice's largest weight
     int below[MAXSLICES];        // bins from the row's first to the slice's first
     u64 kept[MAXSLICES];         // kept weight per slice
@@ -759,9 +763,9 @@ __device__ __forceinline__ bool pick_row(const SampleProblem &P, const Scan &L, 
         st[i] = SliceStat{0, 0, 0, 0, 0};
         if (tid + i * NT < L.slices) st[i] = L.stat[(size_t)r * L.slices + tid + i * NT];
     }
-    constexpr int MOST = MAXV / UNIT / NT;  // groups of four pieces per thread
-    static_assert(SHORTV / (4 * SHORT) <= MOST * NT, "pieces");
-    const int groups = L.pieces / 4;
+    constexpr int MOST = MAXV / PIECE / 8 / NT;  // groups of eight pieces per thread
+    static_assert(SHORTV / SHORT <= 8 * MOST * NT, "pieces");
+    const int groups = L.pieces / 8;
     u32x4 tops[MOST];
     const u32x4 *all_tops = reinterpret_cast<const u32x4 *>(L.tops + (size_t)r * L.pieces);
 #pragma unroll
@@ -792,6 +796,7 @@ __device__ __forceinline__ bool pick_row(const SampleProblem &P, const Scan &L, 
         S.ntodo = S.nlist = 0;
         S.lo_bin = S.hi_bin = HB;
     }
+    if (tid < SLICE / UNIT) S.unit[tid] = S.last[tid] = 0;
     __syncthreads();
     bad = top = finite = 0;
 #pragma unroll
@@ -827,8 +832,9 @@ __device__ __forceinline__ bool pick_row(const SampleProblem &P, const Scan &L, 
     uint32_t low = kLowest, high = 0xffffffffu;
     u64 total = 0, goal = 0, sure_mass = 0;
     bool bounded = false;  // the bracket ends where min-p does: top-p need not cut inside it
+    const double to_one = W.one / (double)(1ull << kHistShift);
     auto to_row = [&](u64 x, int s) {  // a slice's weight in the row's fixed point
-        return (u64)rint((double)x * S.scale[s] * (W.one / (double)(1ull << kHistShift)));
+        return (u64)rint((double)x * S.scale[s] * to_one);
     };
     if (rules.whole) {
         high = kLowest;
@@ -847,18 +853,22 @@ __device__ __forceinline__ bool pick_row(const SampleProblem &P, const Scan &L, 
         // the row's histogram, a bin per thread, and its running sum
         const u64 *hist = L.hist + (size_t)r * L.slices * HB;
         constexpr int AHEAD = 8;
-        u64 h = 0;
+        double weight = 0.0;
+#pragma unroll 1
         for (int s0 = 0; s0 < L.slices; s0 += AHEAD) {
             u64 x[AHEAD];
+            int b[AHEAD];
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) {
-                const int s = min(s0 + i, L.slices - 1), b = s0 + i < L.slices ? tid - S.below[s] : -1;
-                x[i] = b >= 0 && b < HB - 1 ? hist[(size_t)s * HB + b] : 0;
+                const int s = min(s0 + i, L.slices - 1);
+                b[i] = s0 + i < L.slices ? tid - S.below[s] : -1;
+                x[i] = hist[(size_t)s * HB + min(max(b[i], 0), HB - 1)];
             }
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i)
-                if (x[i]) h += to_row(x[i], min(s0 + i, L.slices - 1));
+                if (b[i] >= 0 && b[i] < HB - 1) weight += (double)x[i] * S.scale[min(s0 + i, L.slices - 1)];
         }
+        const u64 h = (u64)rint(weight * to_one);
         u64 all;
         const u64 before = scan(h, all), run = before + h;
         int lo_bin = HB, hi_bin = HB;
@@ -888,22 +898,23 @@ __device__ __forceinline__ bool pick_row(const SampleProblem &P, const Scan &L, 
         high = first_key(first - (float)hi_bin + 1.f, per);
         if (tid == hi_bin) S.at = before;
         // the sure weight per slice
+#pragma unroll 1
         for (int s0 = wave; s0 < L.slices; s0 += NW * 4) {
-            u64 x[4];
+            u64 x[4][HB / 64];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int s = min(s0 + i * NW, L.slices - 1), most = min(hi_bin - S.below[s], HB - 1);
-                x[i] = 0;
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int j = 0; j < HB / 64; ++j)
-                    if (lane + 64 * j < most) x[i] += hist[(size_t)s * HB + lane + 64 * j];
-            }
+                for (int j = 0; j < HB / 64; ++j) x[i][j] = hist[(size_t)min(s0 + i * NW, L.slices - 1) * HB + lane + 64 * j];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int s = s0 + i * NW;
                 if (s >= L.slices) break;
-                const u64 y = wave_sum(x[i]);
-                if (lane == 0) S.kept[s] = to_row(y, s);
+                const int most = min(hi_bin - S.below[s], HB - 1);
+                u64 sum = 0;
+#pragma unroll
+                for (int j = 0; j < HB / 64; ++j) sum += lane + 64 * j < most ? x[i][j] : 0;
+                sum = wave_sum(sum);
+                if (lane == 0) S.kept[s] = to_row(sum, s);
             }
         }
         __syncthreads();
@@ -911,99 +922,111 @@ __device__ __forceinline__ bool pick_row(const SampleProblem &P, const Scan &L, 
     } else if (k <= L.pieces) {
         // at least k tokens reach the k-th largest of the pieces' maxima; its upper 16 bits do
         uint32_t prefix = 0;
-        for (int bit = 30; bit >= 16; bit -= 2) {
-            u64 counts = 0;
+#pragma unroll 1
+        for (int bit = 14; bit >= 0; bit -= 2) {
+            uint32_t reach[3] = {0, 0, 0};
 #pragma unroll
             for (int i = 0; i < MOST; ++i)
                 if (i * NT < groups) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
+                    for (int j = 0; j < 8; ++j) {
+                        const uint32_t t = tops[i][j / 2] >> (j % 2 * 16) & 0xffffu;
 #pragma unroll
-                        for (int c = 1; c < 4; ++c)
-                            counts += (u64)__popcll(__ballot(tops[i][j] >= (prefix | (uint32_t)c << bit))) << (21 * (c - 1));
+                        for (int c = 0; c < 3; ++c)
+                            reach[c] += (uint32_t)__popcll(__ballot(t >= (prefix | (uint32_t)(c + 1) << bit)));
+                    }
                 }
-            if (lane == 0) S.wave[scan.turn][wave] = counts;
+            if (lane == 0) S.wave[scan.turn][wave] = (u64)reach[0] | (u64)reach[1] << 21 | (u64)reach[2] << 42;
             __syncthreads();
-            counts = 0;
+            u64 counts = 0;
 #pragma unroll
             for (int w = 0; w < NW; ++w) counts += S.wave[scan.turn][w];
             scan.turn ^= 1;
             const int c = ((int)(counts & 0x1fffff) >= k) + ((int)(counts >> 21 & 0x1fffff) >= k) + ((int)(counts >> 42) >= k);
             prefix |= (uint32_t)c << bit;
         }
+        prefix <<= 16;
         low = max(prefix, kLowest);
     }
-    // units that hold tokens of the bracket, and these
+    // pieces that hold tokens of the bracket, and these
     uint32_t nsure = finite;
     int nlist = 0, n = 0;  // n: kept tokens of the list
     const u64 *list = S.list;
     if (!rules.whole) {
+        const uint32_t least = low >> 16;
 #pragma unroll
-        for (int i = 0; i < MOST; ++i) {
-            if (L.piece != PIECE || i * NT >= L.units) break;
-            const int unit = tid + i * NT;
-            const uint32_t t = max(max(tops[i][0], tops[i][1]), max(tops[i][2], tops[i][3]));
-            const bool in = unit < L.units && t >= low;
-            const u64 vote = __ballot(in);
-            uint32_t base = 0;
-            if (vote && lane == 0) base = atomicAdd(&S.ntodo, (uint32_t)__popcll(vote));
-            base = (uint32_t)__builtin_amdgcn_readfirstlane((int)base) + __popcll(vote & ((1ull << lane) - 1));
-            if (in) S.todo[base] = (uint16_t)unit;
-        }
+        for (int i = 0; i < MOST; ++i)
+            if (i * NT < groups) {
+                uint32_t mine = 0;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) mine += (tops[i][j / 2] >> (j % 2 * 16) & 0xffffu) >= least;
+                const uint32_t run = (uint32_t)wave_scan(mine);
+                uint32_t at = 0;
+                if (lane == 63 && run) at = atomicAdd(&S.ntodo, run);
+                at = (uint32_t)__builtin_amdgcn_readlane((int)at, 63) + run - mine;
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if ((tops[i][j / 2] >> (j % 2 * 16) & 0xffffu) >= least) {
+                        if (at < MAXTODO) S.todo[at] = (uint16_t)(8 * (tid + i * NT) + j);
+                        ++at;
+                    }
+            }
         __syncthreads();
-        const int ntodo = L.piece == PIECE ? (int)S.ntodo : L.units;  // (a group of short pieces is no unit)
-        nsure = 0;
-        // the bracket as logits: comparisons give the masks (nothing is >= NaN; -0 equals 0)
+        const bool every = S.ntodo > MAXTODO;
+        const int ntodo = every ? L.pieces : (int)S.ntodo;
+        // the bracket as logits (nothing is >= NaN; -0 equals 0)
         const float from = logit_of(low), to = logit_of(high);
-        constexpr int AHEAD = 8;  // units in flight per wave, twice
+        const int lanes = L.piece / 4, per_wave = 64 / lanes, sub = lane / lanes, at0 = lane % lanes * 4;
+        constexpr int AHEAD = 4;  // loads in flight per lane, twice
         struct Batch {
-            int unit[AHEAD];
+            int e[AHEAD];
             f32x4 z[AHEAD];
         };
         auto fetch = [&](int q0, Batch &b) {
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) {
-                const int q = q0 + i * NW;
-                b.unit[i] = q >= ntodo ? -1 : L.piece == PIECE ? __builtin_amdgcn_readfirstlane((int)S.todo[q]) : q;
-                if (b.unit[i] >= 0) b.z[i] = load4<DT>(row, b.unit[i] * UNIT + lane * 4, P.V);
+                const int q = (q0 + i * NW) * per_wave + sub;
+                const int piece = every ? q : (int)S.todo[min(q, MAXTODO - 1)];
+                b.e[i] = q < ntodo ? piece * L.piece + at0 : P.V + 3;  // (load4: -inf)
+                b.z[i] = load4<DT>(row, b.e[i], P.V);
             }
         };
+        uint32_t sure = 0;
         auto take = [&](const Batch &b) {
+            u64 votes[AHEAD][4];
+            uint32_t listed = 0;
 #pragma unroll
-            for (int i = 0; i < AHEAD; ++i) {
-                if (b.unit[i] < 0) break;
-                const int e = b.unit[i] * UNIT + lane * 4;
-                u64 votes[4];
-                uint32_t listed = 0;
+            for (int i = 0; i < AHEAD; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const u64 above = __ballot(b.z[i][j] >= to);
-                    votes[j] = __ballot(b.z[i][j] >= from) & ~above;
-                    nsure += (uint32_t)__popcll(above);
-                    listed += (uint32_t)__popcll(votes[j]);
+                    const bool above = b.z[i][j] >= to;
+                    sure += above;
+                    votes[i][j] = __ballot(b.z[i][j] >= from && !above);
+                    listed += (uint32_t)__popcll(votes[i][j]);
                 }
-                if (!listed) continue;
-                uint32_t base = 0;
-                if (lane == 0) base = atomicAdd(&S.nlist, listed);
-                base = (uint32_t)__builtin_amdgcn_readfirstlane((int)base);
+            if (!listed) return;
+            uint32_t base = 0;
+            if (lane == 0) base = atomicAdd(&S.nlist, listed);
+            base = (uint32_t)__builtin_amdgcn_readfirstlane((int)base);
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const uint32_t at = base + __popcll(votes[j] & ((1ull << lane) - 1));
-                    if ((votes[j] >> lane & 1) && at < MAXLIST)
-                        S.list[at] = (u64)key_of(b.z[i][j]) << 32 | (uint32_t)~(e + j);
-                    base += (uint32_t)__popcll(votes[j]);
+                    const uint32_t at = base + __popcll(votes[i][j] & ((1ull << lane) - 1));
+                    if ((votes[i][j] >> lane & 1) && at < MAXLIST)
+                        S.list[at] = (u64)key_of(b.z[i][j]) << 32 | (uint32_t)~(b.e[i] + j);
+                    base += (uint32_t)__popcll(votes[i][j]);
                 }
-            }
         };
         Batch one, two;
         fetch(wave, one);
-        for (int q0 = wave; q0 < ntodo; q0 += 2 * NW * AHEAD) {
+        for (int q0 = wave; q0 * per_wave < ntodo; q0 += 2 * NW * AHEAD) {
             fetch(q0 + NW * AHEAD, two);
             take(one);
             fetch(q0 + 2 * NW * AHEAD, one);
             take(two);
         }
-        nsure = (uint32_t)scan.sum(lane == 0 ? nsure : 0);
+        nsure = (uint32_t)scan.sum(sure);
         nlist = (int)S.nlist;
         if (nlist > MAXLIST || (rules.k && nlist < k)) return false;
         if (nlist == 0 && rules.p < 1.f && !bounded) return false;
@@ -1076,29 +1099,36 @@ __device__ __forceinline__ bool pick_row(const SampleProblem &P, const Scan &L, 
         if (key < low || !(key >= high || cut.keeps(key, e))) return 0;
         return W.fixed(key);
     };
-    constexpr int AHEAD = SLICE / UNIT / NW;
-    f32x4 z[AHEAD];
-#pragma unroll
-    for (int i = 0; i < AHEAD; ++i)
-        if (wave + i * NW < units) z[i] = load4<DT>(row, e0 + (wave + i * NW) * UNIT + lane * 4, P.V);
-#pragma unroll
-    for (int i = 0; i < AHEAD; ++i) {
-        if (wave + i * NW >= units) break;
-        const int e = e0 + (wave + i * NW) * UNIT + lane * 4;
-        u64 w = 0;
-        uint32_t last = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t key = key_of(z[i][j]);
-            w += weight(key, e + j);
-            if (key >= kLowest && key >= low && (key >= high || cut.keeps(key, e + j))) last = e + j + 1;
+    if (high == 0xffffffffu) {  // every kept token is in the list
+        for (int i = tid; i < n; i += NT) {
+            const u64 x = list[i];
+            const int e = (int)(uint32_t)~x - e0;
+            if (e < 0 || e >= L.slice) continue;
+            atomicAdd(&S.unit[e / UNIT], W.fixed((uint32_t)(x >> 32)));
+            atomicMax(&S.last[e / UNIT], (uint32_t)~x + 1);
         }
-        w = wave_sum(w);
+    } else {
+        f32x4 z = load4<DT>(row, e0 + wave * UNIT + lane * 4, P.V);
+#pragma unroll 1
+        for (int i = wave; i < units; i += NW) {
+            const f32x4 next = load4<DT>(row, e0 + min(i + NW, units - 1) * UNIT + lane * 4, P.V);
+            const int e = e0 + i * UNIT + lane * 4;
+            u64 w = 0;
+            uint32_t last = 0;
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) last = max(last, (uint32_t)__shfl_xor((int)last, o));
-        if (lane == 0) {
-            S.unit[wave + i * NW] = w;
-            S.last[wave + i * NW] = last;
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t key = key_of(z[j]);
+                w += weight(key, e + j);
+                if (key >= kLowest && key >= low && (key >= high || cut.keeps(key, e + j))) last = e + j + 1;
+            }
+            w = wave_sum(w);
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) last = max(last, (uint32_t)__shfl_xor((int)last, o));
+            if (lane == 0) {
+                S.unit[i] = w;
+                S.last[i] = last;
+            }
+            z = next;
         }
     }
     __syncthreads();
@@ -1216,9 +1246,8 @@ Scan layout(const SampleProblem &p, char *ws, size_t &bytes) {
     const int large = (p.V + SLICE - 1) / SLICE;
     L.slice = (long long)p.R * large < 2 * kCus && p.V <= 2048 * MAXSLICES ? 2048 : SLICE;
     L.slices = (p.V + L.slice - 1) / L.slice;
-    L.units = (p.V + UNIT - 1) / UNIT;
-    L.piece = L.units * UNIT <= SHORTV ? SHORT : PIECE;
-    L.pieces = L.units * UNIT / L.piece;
+    L.piece = p.V <= SHORTV ? SHORT : PIECE;
+    L.pieces = (p.V + 8 * L.piece - 1) / (8 * L.piece) * 8;  // (a slice is a multiple of that)
     size_t off = 0;
     auto take = [&](size_t n) {
         char *at = ws ? ws + off : nullptr;
@@ -1227,7 +1256,7 @@ Scan layout(const SampleProblem &p, char *ws, size_t &bytes) {
     };
     const size_t R = (size_t)p.R;
     L.stat = (SliceStat *)take(R * L.slices * sizeof(SliceStat));
-    L.tops = (uint32_t *)take(R * L.pieces * 4);
+    L.tops = (uint16_t *)take(R * L.pieces * 2);
     L.hist = (u64 *)take(R * L.slices * HB * sizeof(u64));
     L.spread = (Spread *)take(R * sizeof(Spread));
     bytes = off ? off : 256;
@@ -1239,7 +1268,7 @@ hipError_t launch(const SampleProblem &p, char *ws, hipStream_t st) {
     const int idbits = bits_of((uint32_t)(p.V - 1));
     // V weights of at most 2^shift stay below 2^62; a weight is a whole number in a double
     const int shift = idbits > 12 ? 62 - idbits : 50;
-    if (p.V > MAXV) {
+    if (p.V > MAXV || p.V < 4) {
         hipLaunchKernelGGL((search_kernel<DT>), dim3(p.R), dim3(NT), 0, st, p, shift, idbits);
         return hipGetLastError();
     }
@@ -1261,7 +1290,7 @@ hipError_t launch(const SampleProblem &p, char *ws, hipStream_t st) {
 }  // namespace
 
 size_t sample_workspace(const SampleProblem &p) {
-    if (p.V > MAXV) return 256;
+    if (p.V > MAXV || p.V < 4) return 256;
     size_t bytes;
     layout(p, nullptr, bytes);
     return bytes;
