@@ -28,7 +28,7 @@ namespace {
 
 typedef unsigned long long u64;
 
-constexpr int NT = 256;              // threads of a row's workgroup
+constexpr int NT = 512;              // threads of a row's workgroup
 constexpr int NW = NT / 64;
 constexpr int BITS = 11;             // of a key per search level
 constexpr int BINS = 1 << BITS;
@@ -632,7 +632,8 @@ struct PickLds {
     u64 kept[MAXSLICES];         // kept weight per slice
     u64 unit[SLICE / UNIT];      // and per unit of a slice, with the number of its last kept token + 1
     uint32_t last[SLICE / UNIT];
-    u64 wave[2][NW];             // of block_scan
+    u64 wave[2][NW];        // of BlockScan
+    u64 reach[8];                // three counts of pieces' maxima for each pair of bits
     u64 at;
     uint32_t top[NW], bad[NW], finite[NW];
     uint32_t ntodo, nlist, pick, lo_bin, hi_bin;
@@ -756,21 +757,26 @@ __device__ __forceinline__ bool pick_row(const SampleProblem &P, const Scan &L, 
     const char *row = row_of<DT>(P, r);
     BlockScan scan{S};
     // everything that is read at an address known from the start: one trip to memory
-    constexpr int SPT = MAXSLICES / NT;  // slices per thread
+    constexpr int SPT = (MAXSLICES + NT - 1) / NT;  // slices per thread
     SliceStat st[SPT];
 #pragma unroll
     for (int i = 0; i < SPT; ++i) {
         st[i] = SliceStat{0, 0, 0, 0, 0};
         if (tid + i * NT < L.slices) st[i] = L.stat[(size_t)r * L.slices + tid + i * NT];
     }
-    constexpr int MOST = MAXV / PIECE / 8 / NT;  // groups of eight pieces per thread
-    static_assert(SHORTV / SHORT <= 8 * MOST * NT, "pieces");
-    const int groups = L.pieces / 8;
-    u32x4 tops[MOST];
-    const u32x4 *all_tops = reinterpret_cast<const u32x4 *>(L.tops + (size_t)r * L.pieces);
+    constexpr int GROUP = 2048 / NT;  // pieces of a group
+    constexpr int MOST = MAXV / PIECE / GROUP / NT;  // groups per thread
+    static_assert(SHORTV / SHORT <= GROUP * MOST * NT, "pieces");
+    struct alignas(GROUP * 2) Group {
+        uint32_t two[GROUP / 2];
+        __device__ __forceinline__ uint32_t operator[](int j) const { return two[j / 2] >> (j % 2 * 16) & 0xffffu; }
+    };
+    const int groups = L.pieces / GROUP;
+    Group tops[MOST];
+    const Group *all_tops = reinterpret_cast<const Group *>(L.tops + (size_t)r * L.pieces);
 #pragma unroll
     for (int i = 0; i < MOST; ++i) {
-        tops[i] = u32x4{0, 0, 0, 0};
+        tops[i] = Group{};
         if (tid + i * NT < groups) tops[i] = all_tops[tid + i * NT];
     }
     const Rules rules(P, r);
@@ -797,6 +803,7 @@ __device__ __forceinline__ bool pick_row(const SampleProblem &P, const Scan &L, 
         S.lo_bin = S.hi_bin = HB;
     }
     if (tid < SLICE / UNIT) S.unit[tid] = S.last[tid] = 0;
+    if (tid < 8) S.reach[tid] = 0;
     __syncthreads();
     bad = top = finite = 0;
 #pragma unroll
@@ -850,25 +857,30 @@ __device__ __forceinline__ bool pick_row(const SampleProblem &P, const Scan &L, 
         for (int i = 0; i < SPT; ++i)
             if (tid + i * NT < L.slices) mine += to_row(st[i].mass, tid + i * NT);
         total = scan.sum(mine);
-        // the row's histogram, a bin per thread, and its running sum
+        // the row's histogram, a bin of a share of the slices per thread, and its running sum
         const u64 *hist = L.hist + (size_t)r * L.slices * HB;
         constexpr int AHEAD = 8;
+        const int bin = tid % HB;
         double weight = 0.0;
 #pragma unroll 1
-        for (int s0 = 0; s0 < L.slices; s0 += AHEAD) {
+        for (int s0 = tid / HB * AHEAD; s0 < L.slices; s0 += NT / HB * AHEAD) {
             u64 x[AHEAD];
             int b[AHEAD];
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) {
                 const int s = min(s0 + i, L.slices - 1);
-                b[i] = s0 + i < L.slices ? tid - S.below[s] : -1;
+                b[i] = s0 + i < L.slices ? bin - S.below[s] : -1;
                 x[i] = hist[(size_t)s * HB + min(max(b[i], 0), HB - 1)];
             }
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i)
                 if (b[i] >= 0 && b[i] < HB - 1) weight += (double)x[i] * S.scale[min(s0 + i, L.slices - 1)];
         }
-        const u64 h = (u64)rint(weight * to_one);
+        double *part = reinterpret_cast<double *>(S.list);
+        part[tid] = weight;
+        __syncthreads();
+        for (int t = tid + HB; t < NT; t += HB) weight += part[t];
+        const u64 h = tid < HB ? (u64)rint(weight * to_one) : 0;
         u64 all;
         const u64 before = scan(h, all), run = before + h;
         int lo_bin = HB, hi_bin = HB;
@@ -929,19 +941,14 @@ __device__ __forceinline__ bool pick_row(const SampleProblem &P, const Scan &L, 
             for (int i = 0; i < MOST; ++i)
                 if (i * NT < groups) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const uint32_t t = tops[i][j / 2] >> (j % 2 * 16) & 0xffffu;
+                    for (int j = 0; j < GROUP; ++j)
 #pragma unroll
                         for (int c = 0; c < 3; ++c)
-                            reach[c] += (uint32_t)__popcll(__ballot(t >= (prefix | (uint32_t)(c + 1) << bit)));
-                    }
+                            reach[c] += (uint32_t)__popcll(__ballot(tops[i][j] >= (prefix | (uint32_t)(c + 1) << bit)));
                 }
-            if (lane == 0) S.wave[scan.turn][wave] = (u64)reach[0] | (u64)reach[1] << 21 | (u64)reach[2] << 42;
+            if (lane == 0) atomicAdd(&S.reach[bit / 2], (u64)reach[0] | (u64)reach[1] << 21 | (u64)reach[2] << 42);
             __syncthreads();
-            u64 counts = 0;
-#pragma unroll
-            for (int w = 0; w < NW; ++w) counts += S.wave[scan.turn][w];
-            scan.turn ^= 1;
+            const u64 counts = S.reach[bit / 2];
             const int c = ((int)(counts & 0x1fffff) >= k) + ((int)(counts >> 21 & 0x1fffff) >= k) + ((int)(counts >> 42) >= k);
             prefix |= (uint32_t)c << bit;
         }
@@ -959,15 +966,15 @@ __device__ __forceinline__ bool pick_row(const SampleProblem &P, const Scan &L, 
             if (i * NT < groups) {
                 uint32_t mine = 0;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) mine += (tops[i][j / 2] >> (j % 2 * 16) & 0xffffu) >= least;
+                for (int j = 0; j < GROUP; ++j) mine += tops[i][j] >= least;
                 const uint32_t run = (uint32_t)wave_scan(mine);
                 uint32_t at = 0;
                 if (lane == 63 && run) at = atomicAdd(&S.ntodo, run);
                 at = (uint32_t)__builtin_amdgcn_readlane((int)at, 63) + run - mine;
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if ((tops[i][j / 2] >> (j % 2 * 16) & 0xffffu) >= least) {
-                        if (at < MAXTODO) S.todo[at] = (uint16_t)(8 * (tid + i * NT) + j);
+                for (int j = 0; j < GROUP; ++j)
+                    if (tops[i][j] >= least) {
+                        if (at < MAXTODO) S.todo[at] = (uint16_t)(GROUP * (tid + i * NT) + j);
                         ++at;
                     }
             }

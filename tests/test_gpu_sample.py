@@ -134,6 +134,21 @@ def test_flat_rows(V, spread):
     Call(z, uniforms(R, 2), top_p=top_p, top_k=top_k).run().check()
 
 
+@pytest.mark.parametrize("V", [3, 701, 9001, 20003])
+def test_more_rows_than_compute_units(V):
+    """Deep, flat, mixed and masked rows by the hundred (a row has fewer threads there)."""
+    R = 300
+    z = logits(R, V, 15, 2.0)
+    z[5::7] *= 0.02
+    z[3::11, ::2] = -np.inf
+    z[4::50] = -np.inf
+    rules = mixed(R, 16)
+    rules["top_k"][::9] = V // 2
+    rules["top_p"][1::8], rules["top_k"][1::8], rules["min_p"][1::8] = 0.97, 0, 0
+    Call(z, uniforms(R, 17), **rules).run().check(range(0, R, 3))
+    Call(z, uniforms(R, 18), top_p=np.linspace(0, 1, R).astype(np.float32)).run().check(range(1, R, 3))
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("V", [700, 20003])
 def test_masks_and_values_at_the_ends(V, dtype):
