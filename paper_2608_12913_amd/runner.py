@@ -127,3 +127,98 @@ class DeviceProblem:
                        row_argmax_expert=self.row_argmax_expert.cpu().numpy(),
                        row_kl=self.row_kl.cpu().numpy())
         return out
+
+
+class DraftHead:
+    """A drafter's LM head held in 8-bit codes, with the buffers for up to `max_rows` hidden states:
+    a token per row, drawn with that row's rules, and the distribution it was drawn from.
+
+    w: [V, d] bf16 or fp32 (a tensor, or numpy as in :class:`DeviceProblem`); its codes and scales
+    are made here, once.  A step is three kernels' calls (codes of the hidden states, logits,
+    sampling); it allocates nothing and can be captured into a graph.  Calls share the buffers: run
+    them in stream order.
+    """
+
+    def __init__(self, w, bias=None, *, max_rows, logits_dtype="f32", device="cuda:0"):
+        self.device = torch.device(device)
+        w = (w if torch.is_tensor(w) else _dev(w, self.device)).to(self.device).contiguous()
+        self.V, self.d = w.shape
+        self.max_rows, self.logits_dtype = int(max_rows), logits_dtype
+        if bias is not None:
+            bias = torch.as_tensor(bias).to(self.device, torch.float32).contiguous()
+            if bias.shape != (self.V,):
+                raise ValueError(f"bias {tuple(bias.shape)} for {self.V} tokens")
+        self.bias = bias
+        groups = -(-self.d // 128)
+        u8 = dict(dtype=torch.uint8, device=self.device)
+        f32 = dict(dtype=torch.float32, device=self.device)
+        self.w, self.w_scale = torch.empty(self.V, self.d, **u8), torch.empty(-(-self.V // 128), groups, **f32)
+        self.h, self.h_scale = torch.empty(self.max_rows, self.d, **u8), torch.empty(self.max_rows, groups, **f32)
+        self.logits = torch.empty(self.max_rows, self.V, device=self.device,
+                                  dtype=torch.bfloat16 if logits_dtype == "bf16" else torch.float32)
+        self.ws_bytes = dcd.sample_workspace_bytes(dcd.make_sample_problem(self.max_rows, self.V, logits_dtype))
+        if self.ws_bytes == 0:
+            raise dcd.DcdError(dcd.DCD_ERR_SHAPE)
+        self.workspace = torch.empty(self.ws_bytes, **u8)
+        stream = torch.cuda.current_stream(self.device)
+        dcd.quantize_fp8(w, self.w, self.w_scale, rows=self.V, cols=self.d, dtype=self._name(w), block_rows=128,
+                         stream=stream)
+        stream.synchronize()  # `w` may go; any stream may use the codes
+
+    @staticmethod
+    def _name(t) -> str:
+        if t.dtype not in (torch.bfloat16, torch.float32):
+            raise ValueError(f"{t.dtype}: bf16 or fp32")
+        return "bf16" if t.dtype == torch.bfloat16 else "f32"
+
+    def _take(self, name, t, shape, dtype=None):
+        """`t` as the library takes it: on this device, contiguous, of this shape and type."""
+        if t is None:
+            return None
+        if (t.device != self.w.device or tuple(t.shape) != shape or not t.is_contiguous()
+                or (dtype is not None and t.dtype != dtype)):
+            raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}, wanted "
+                             f"{dtype or 'bf16 or fp32'} {shape}, contiguous, on {self.w.device}")
+        return t
+
+    def launch(self, h, u, tokens, probs=None, *, temperature=None, top_k=None, top_p=None,
+               min_p=None, logprob=None, kept=None, stream=None) -> None:
+        """Enqueue one step on `stream` (default: torch's current stream): h [rows, d] bf16 or fp32,
+        u [rows] and the rules (each None or [rows]); tokens int32 and, where given, probs [rows, V], logprob and
+        kept are written.  tokens and probs may be a :class:`DeviceProblem`'s tokens and
+        draft_probs, where row b * N + i proposes node i of sequence b."""
+        rows = int(h.shape[0])
+        if rows > self.max_rows:
+            raise ValueError(f"{rows} rows, room for {self.max_rows}")
+        f32, i32 = torch.float32, torch.int32
+        h = self._take("h", h, (rows, self.d))
+        u = self._take("u", u, (rows,), f32)
+        tokens = self._take("tokens", tokens.view(-1), (rows,), i32)
+        rules = [self._take(n, t, (rows,), d) for n, t, d in
+                 (("temperature", temperature, f32), ("top_k", top_k, i32), ("top_p", top_p, f32), ("min_p", min_p, f32))]
+        outs = [self._take(n, t, s, d) for n, t, s, d in
+                (("probs", probs, (rows, self.V), f32), ("logprob", logprob, (rows,), f32), ("kept", kept, (rows,), i32))]
+        if stream is None:
+            stream = torch.cuda.current_stream(self.device)
+        dcd.quantize_fp8(h, self.h, self.h_scale, rows=rows, cols=self.d, dtype=self._name(h), stream=stream)
+        dcd.logits_fp8(dcd.make_fp8_problem(rows, self.V, self.d, self.logits_dtype),
+                       dcd.make_fp8_inputs(self.h, self.h_scale, self.w, self.w_scale, self.bias),
+                       self.logits, stream)
+        dcd.sample(dcd.make_sample_problem(rows, self.V, self.logits_dtype),
+                   dcd.make_sample_inputs(self.logits, u, *rules), dcd.make_sample_outputs(tokens, *outs),
+                   self.workspace, self.ws_bytes, stream)
+
+    def propose(self, h, u, *, want_probs=True, **rules) -> dict:
+        """One synchronous step on numpy (or torch) inputs; returns host copies of the outputs."""
+        h = (h if torch.is_tensor(h) else _dev(h, self.device)).to(self.device).contiguous()
+        rows = int(h.shape[0])
+        dv = lambda a, t: None if a is None else torch.as_tensor(a).to(self.device, t).contiguous()  # noqa: E731
+        rules = {n: dv(a, torch.int32 if n == "top_k" else torch.float32) for n, a in rules.items()}
+        i32, f32 = dict(dtype=torch.int32, device=self.device), dict(dtype=torch.float32, device=self.device)
+        out = dict(tokens=torch.empty(rows, **i32), kept=torch.empty(rows, **i32), logprob=torch.empty(rows, **f32))
+        if want_probs:
+            out["probs"] = torch.empty(rows, self.V, **f32)
+        self.launch(h, dv(u, torch.float32), out["tokens"], out.get("probs"), logprob=out["logprob"],
+                    kept=out["kept"], **rules)
+        torch.cuda.synchronize(self.device)
+        return {n: t.cpu().numpy() for n, t in out.items()}
