@@ -459,7 +459,7 @@ struct Scan {
     int slice, slices, piece, pieces;  // logits per slice and piece; slices and pieces of a row
     SliceStat *stat;                   // [R][slices]
     uint16_t *tops;                    // [R][pieces]: upper half of the key of each piece's largest logit
-    u64 *hist;                         // [R][slices][HB]: weights at 2^kHistShift, the last bin: the rest
+    u64 *hist;                         // [R][slices][HB]: weights at 2^kHistShift (the last bin stays 0)
     Spread *spread;                    // [R]
 };
 
@@ -607,7 +607,8 @@ __global__ __launch_bounds__(ST) void scan_kernel(SampleProblem P, Scan L) {
                 if (key < kLowest) continue;
                 const u64 w = W.fixed(key);
                 m += w;
-                if (!rules.whole && w) atomicAdd(&hist[(int)fminf(first - bin_of(z[i][j], per), HB - 1.f)], w);
+                const float bin = first - bin_of(z[i][j], per);
+                if (!rules.whole && w && bin < HB - 1.f) atomicAdd(&hist[(int)bin], w);
             }
         m = wave_sum(m);
         if (lane == 0) wmass[wave] = m;
