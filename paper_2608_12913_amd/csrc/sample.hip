@@ -712,7 +712,7 @@ __device__ __forceinline__ u64 *sort_list(u64 *list, int n) {
     for (int k = 2; k <= size; k <<= 1)
         for (int j = k >> 1; j > 0; j >>= 1) {
             for (int t = tid; t < size / 2; t += NT) {
-                const int i = 2 * j * (t / j) + t % j;
+                const int i = 2 * (t & -j) + (t & (j - 1));
                 const u64 a = list[i], b = list[i + j];
                 if ((a < b) == ((i & k) == 0)) {
                     list[i] = b;
