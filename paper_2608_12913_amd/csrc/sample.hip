@@ -853,39 +853,41 @@ __device__ __forceinline__ bool pick_row(const SampleProblem &P, const Scan &L, 
     } else if (rules.k == 0) {
         if (!(fabsf(first) < kBinLimit)) return false;
         __syncthreads();
-        u64 mine = 0;
-#pragma unroll
-        for (int i = 0; i < SPT; ++i)
-            if (tid + i * NT < L.slices) mine += to_row(st[i].mass, tid + i * NT);
-        total = scan.sum(mine);
-        // the row's histogram, a bin of a share of the slices per thread, and its running sum
         const u64 *hist = L.hist + (size_t)r * L.slices * HB;
-        constexpr int AHEAD = 8;
-        const int bin = tid % HB;
-        double weight = 0.0;
-#pragma unroll 1
-        for (int s0 = tid / HB * AHEAD; s0 < L.slices; s0 += NT / HB * AHEAD) {
-            u64 x[AHEAD];
-            int b[AHEAD];
-#pragma unroll
-            for (int i = 0; i < AHEAD; ++i) {
-                const int s = min(s0 + i, L.slices - 1);
-                b[i] = s0 + i < L.slices ? bin - S.below[s] : -1;
-                x[i] = hist[(size_t)s * HB + min(max(b[i], 0), HB - 1)];
-            }
-#pragma unroll
-            for (int i = 0; i < AHEAD; ++i)
-                if (b[i] >= 0 && b[i] < HB - 1) weight += (double)x[i] * S.scale[min(s0 + i, L.slices - 1)];
-        }
-        double *part = reinterpret_cast<double *>(S.list);
-        part[tid] = weight;
-        __syncthreads();
-        for (int t = tid + HB; t < NT; t += HB) weight += part[t];
-        const u64 h = tid < HB ? (u64)rint(weight * to_one) : 0;
-        u64 all;
-        const u64 before = scan(h, all), run = before + h;
         int lo_bin = HB, hi_bin = HB;
+        u64 before = 0;
         if (rules.p < 1.f) {
+            u64 mine = 0;
+#pragma unroll
+            for (int i = 0; i < SPT; ++i)
+                if (tid + i * NT < L.slices) mine += to_row(st[i].mass, tid + i * NT);
+            total = scan.sum(mine);
+            // the row's histogram, a bin of a share of the slices per thread, and its running sum
+            constexpr int AHEAD = 8;
+            const int bin = tid % HB;
+            double weight = 0.0;
+#pragma unroll 1
+            for (int s0 = tid / HB * AHEAD; s0 < L.slices; s0 += NT / HB * AHEAD) {
+                u64 x[AHEAD];
+                int b[AHEAD];
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i) {
+                    const int s = min(s0 + i, L.slices - 1);
+                    b[i] = s0 + i < L.slices ? bin - S.below[s] : -1;
+                    x[i] = hist[(size_t)s * HB + min(max(b[i], 0), HB - 1)];
+                }
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i)
+                    if (b[i] >= 0 && b[i] < HB - 1) weight += (double)x[i] * S.scale[min(s0 + i, L.slices - 1)];
+            }
+            double *part = reinterpret_cast<double *>(S.list);
+            part[tid] = weight;
+            __syncthreads();
+            for (int t = tid + HB; t < NT; t += HB) weight += part[t];
+            const u64 h = tid < HB ? (u64)rint(weight * to_one) : 0;
+            u64 all;
+            before = scan(h, all);
+            const u64 run = before + h;
             goal = (u64)ceil((double)rules.p * (double)total);
             goal = goal < 1 ? 1 : goal > total ? total : goal;
             // (slices and bins were rounded apart: a billionth is far more than that)
@@ -910,14 +912,17 @@ __device__ __forceinline__ bool pick_row(const SampleProblem &P, const Scan &L, 
         low = first_key(first - (float)lo_bin, per);
         high = first_key(first - (float)hi_bin + 1.f, per);
         if (tid == hi_bin) S.at = before;
-        // the sure weight per slice
+        // the sure weight per slice: its bins before the row's hi_bin
 #pragma unroll 1
         for (int s0 = wave; s0 < L.slices; s0 += NW * 4) {
             u64 x[4][HB / 64];
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int j = 0; j < HB / 64; ++j) x[i][j] = hist[(size_t)min(s0 + i * NW, L.slices - 1) * HB + lane + 64 * j];
+                for (int j = 0; j < HB / 64; ++j) {
+                    x[i][j] = 0;
+                    if (64 * j < hi_bin) x[i][j] = hist[(size_t)min(s0 + i * NW, L.slices - 1) * HB + lane + 64 * j];
+                }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int s = s0 + i * NW;
