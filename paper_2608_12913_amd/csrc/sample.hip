@@ -599,15 +599,17 @@ __global__ __launch_bounds__(ST) void scan_kernel(SampleProblem P, Scan L) {
         const Weights W(top, rules.T, kHistShift, table);
         u64 m = 0;
         const float per = 16.f / rules.T, first = bin_of(logit_of(top), per);
+        // with min-p alone, only the bins above its bound are read (4: for the roundings on the way to it)
+        const float most = rules.p == 1.f && !rules.whole ? fminf(4.f - 16.f * logf(rules.m), HB - 1.f) : INFINITY;
 #pragma unroll
         for (int i = 0; i < EPT / 4; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const uint32_t key = key_of(z[i][j]);
-                if (key < kLowest) continue;
+                const float bin = first - bin_of(z[i][j], per);
+                if (key < kLowest || bin >= most) continue;
                 const u64 w = W.fixed(key);
                 m += w;
-                const float bin = first - bin_of(z[i][j], per);
                 if (!rules.whole && w && bin < HB - 1.f) atomicAdd(&hist[(int)bin], w);
             }
         m = wave_sum(m);
