@@ -14,13 +14,26 @@
 // call and a border between two tokens is where 64-bit arithmetic puts it.
 //
 // Two launches, or three.  scan_kernel reads the logits once, in slices of 2,048 or 8,192 spread over
-// the chip: the largest logit of every 64 and, where no top-k bounds the row, a histogram of the
-// slice's weight; it writes the zeros of the probabilities.  pick_kernel has a workgroup per row, which
-// brackets the cutoff from these to a few hundred tokens, reads again only the pieces that can hold
-// one, puts what lies inside the bracket in order, and draws.  What lies surely above the bracket
-// (rows without top-k) is spread over the chip once more for its dense probabilities
-// (spread_kernel).  Where the bracket fails (too many tokens inside, a top-k larger than the
-// number of pieces) the row's workgroup searches the logits themselves (search_row).
+// the chip: the largest logit of every 64 (of fewer in short vocabularies) and, where no top-k bounds
+// the row, a histogram of the slice's weight; it writes the zeros of the probabilities.  pick_kernel
+// has a workgroup per row, which brackets the cutoff from these to a few hundred tokens, reads again
+// only the pieces that can hold one, puts what lies inside the bracket in order, and draws.  What lies
+// surely above the bracket (rows without top-k) is spread over the chip once more for its dense
+// probabilities (spread_kernel).  Where the bracket fails (too many tokens inside, a top-k larger
+// than the number of pieces) the row's workgroup searches the logits themselves (search_row), as it
+// does for vocabularies under 4 or above 2^20 tokens.
+//
+// What bounds it, rows of 128,256 fp32 logits without dense probabilities, us (of which a streaming
+// read needs 0.1, 10 and 77):
+//                         1 row   128 rows   1,024 rows
+//   argmax                 19.6     33         130
+//   top-k 50               20.3     34         134    memory, and 20 us of a row's dependent steps
+//   min-p 0.05             22.2     40         161
+//   no rule                12.2     41         207    a 64-bit exponential per logit
+//   top-p 0.9              31.5     58         244    the same, and the slices' histograms
+//   top-p 0.9, flat        105      132        443    a bracket of thousands: order, second reading
+// A row by one workgroup from the logits alone, with a radix search of all of them per level, took
+// 301 us (1 row, top-k and top-p) and 2,156 us (1,024 rows of mixed rules, 345 now).
 #include "proposal.h"
 
 namespace dcd {
@@ -28,7 +41,9 @@ namespace {
 
 typedef unsigned long long u64;
 
-constexpr int NT = 512;              // threads of a row's workgroup
+// Threads of a row's workgroup.  256 or 1,024 instead: one row of top-p 42 or 37 us (32 with 512), of a
+// flat nucleus 187 or 101 (117), 512 rows of top-k 64 or 87 (66), of a flat nucleus 295 or 291 (251).
+constexpr int NT = 512;
 constexpr int NW = NT / 64;
 constexpr int BITS = 11;             // of a key per search level
 constexpr int BINS = 1 << BITS;
@@ -426,19 +441,22 @@ __global__ __launch_bounds__(NT) void search_kernel(SampleProblem P, int shift, 
 }
 
 // ---------------------------------------------------------------------------
-// The two launches.
+// The launches.
 
 constexpr int ST = 256;         // threads of a slice's workgroup
-constexpr int PIECE = 64;       // logits per recorded maximum,
-constexpr int SHORT = 4;        // or in vocabularies of up to SHORTV (so that a bracket by top-k stays narrow)
-constexpr int SHORTV = 65536;
-constexpr int UNIT = 256;       // logits read again together
+// Logits per recorded maximum: 4 or 16 where a row still has no more than MANY of those, else 64.  A top-k
+// needs at least k maxima, and its bracket is the narrower the more there are, but each is also looked
+// at: 16 rows of 32,003 with top-k 50 take 19.8 us with pieces of 16, 24.8 with 4, 20.7 with 64 (which a
+// top-k above 501 cannot use, and then the logits are searched: 11 rows of 3,779 took 114 us, 25 with 4).
+constexpr int PIECE = 64;
+constexpr int MANY = 2048;
+constexpr int UNIT = 256;       // logits of a wave's load: the draw goes slice, unit, token
 constexpr int HB = 256;         // histogram bins, 1/16 of a temperature wide, below the slice's largest logit
 constexpr int SLICE = 8192;     // logits per slice (of a dense row's second pass, too)
 constexpr int MAXV = 1 << 20;   // largest vocabulary of this path
 constexpr int MAXLIST = 4096;   // tokens inside a row's bracket
 constexpr int MAXTODO = 4096;   // pieces that may hold one, by number (more: every piece of the row)
-constexpr int MAXCOUNTED = 512;  // up to so many are put in order by counting
+constexpr int MAXCOUNTED = 512;  // up to so many are put in order by counting (240: 5.7 us, sorted in pairs 9)
 constexpr int kHistShift = 50;  // 8,192 weights of a slice stay below 2^63
 constexpr int MAXSLICES = MAXV / SLICE > 512 ? MAXV / SLICE : 512;
 constexpr float kBinLimit = 4194304.f;  // |bin numbers| up to here are exact in fp32
@@ -456,7 +474,7 @@ struct Spread {
 };
 
 struct Scan {
-    int slice, slices, piece, pieces;  // logits per slice and piece; slices and pieces of a row
+    int slice, slices, bits, pieces;  // logits per slice, 2^bits per piece; slices and pieces of a row
     SliceStat *stat;                   // [R][slices]
     uint16_t *tops;                    // [R][pieces]: upper half of the key of each piece's largest logit
     u64 *hist;                         // [R][slices][HB]: weights at 2^kHistShift (the last bin stays 0)
@@ -566,13 +584,8 @@ __global__ __launch_bounds__(ST) void scan_kernel(SampleProblem P, Scan L) {
             finite += key >= kLowest;
         }
         const int e = at + i * ST * 4;
-        if (L.piece == PIECE) {
-#pragma unroll
-            for (int o = 1; o < PIECE / 4; o <<= 1) t = max(t, (uint32_t)__shfl_xor((int)t, o));
-            if (lane % (PIECE / 4) == 0 && e < L.pieces * PIECE) tops[e / PIECE] = (uint16_t)(t >> 16);
-        } else if (e < L.pieces * SHORT) {
-            tops[e / SHORT] = (uint16_t)(t >> 16);
-        }
+        for (int o = 1; o < 1 << (L.bits - 2); o <<= 1) t = max(t, (uint32_t)__shfl_xor((int)t, o));
+        if ((e & ((1 << L.bits) - 1)) == 0 && e >> L.bits < L.pieces) tops[e >> L.bits] = (uint16_t)(t >> 16);
         top = max(top, t);
     }
 #pragma unroll
@@ -706,7 +719,7 @@ __device__ __forceinline__ u64 *sort_list(u64 *list, int n) {
         __syncthreads();
         return list + MAXLIST;
     }
-    int size = 1024;
+    int size = 2 * MAXCOUNTED;
     while (size < n) size <<= 1;
     for (int i = n + tid; i < size; i += NT) list[i] = 0;
     __syncthreads();
@@ -769,7 +782,7 @@ __device__ __forceinline__ bool pick_row(const SampleProblem &P, const Scan &L, 
     }
     constexpr int GROUP = 2048 / NT;  // pieces of a group
     constexpr int MOST = MAXV / PIECE / GROUP / NT;  // groups per thread
-    static_assert(SHORTV / SHORT <= GROUP * MOST * NT, "pieces");
+    static_assert(MANY <= GROUP * MOST * NT, "pieces");
     struct alignas(GROUP * 2) Group {
         uint32_t two[GROUP / 2];
         __device__ __forceinline__ uint32_t operator[](int j) const { return two[j / 2] >> (j % 2 * 16) & 0xffffu; }
@@ -991,7 +1004,8 @@ __device__ __forceinline__ bool pick_row(const SampleProblem &P, const Scan &L, 
         const int ntodo = every ? L.pieces : (int)S.ntodo;
         // the bracket as logits (nothing is >= NaN; -0 equals 0)
         const float from = logit_of(low), to = logit_of(high);
-        const int lanes = L.piece / 4, per_wave = 64 / lanes, sub = lane / lanes, at0 = lane % lanes * 4;
+        const int lane_bits = L.bits - 2, per_wave = 64 >> lane_bits, sub = lane >> lane_bits;
+        const int at0 = (lane & ((1 << lane_bits) - 1)) * 4;
         constexpr int AHEAD = 4;  // loads in flight per lane, twice
         struct Batch {
             int e[AHEAD];
@@ -1002,7 +1016,7 @@ __device__ __forceinline__ bool pick_row(const SampleProblem &P, const Scan &L, 
             for (int i = 0; i < AHEAD; ++i) {
                 const int q = (q0 + i * NW) * per_wave + sub;
                 const int piece = every ? q : (int)S.todo[min(q, MAXTODO - 1)];
-                b.e[i] = q < ntodo ? piece * L.piece + at0 : P.V + 3;  // (load4: -inf)
+                b.e[i] = q < ntodo ? (piece << L.bits) + at0 : P.V + 3;  // (load4: -inf)
                 b.z[i] = load4<DT>(row, b.e[i], P.V);
             }
         };
@@ -1255,14 +1269,17 @@ int bits_of(uint32_t x) {
     return b;
 }
 
-// Slices of 8,192 logits, or of 2,048 where the rows are too few to fill the chip with those.
+// Slices of 8,192 logits, or of 2,048 where the rows are too few to fill the chip with those.  8,192 and
+// 2,048, us, no rule / min-p / top-p: 1 row of 128,256 21 and 12 / 26 and 23 / 34 and 32; 24 rows 23 and 16 /
+// 27 and 26 / 39 and 39; 64 rows 29 and 25 / 31 and 34 / 42 and 47; 128 rows of 32,003 23 and 18 / 27 and 25 /
+// 35 and 33.
 Scan layout(const SampleProblem &p, char *ws, size_t &bytes) {
     Scan L{};
     const int large = (p.V + SLICE - 1) / SLICE;
-    L.slice = (long long)p.R * large < 2 * kCus && p.V <= 2048 * MAXSLICES ? 2048 : SLICE;
+    L.slice = (long long)p.R * large <= 2 * kCus && p.V <= 2048 * MAXSLICES ? 2048 : SLICE;
     L.slices = (p.V + L.slice - 1) / L.slice;
-    L.piece = p.V <= SHORTV ? SHORT : PIECE;
-    L.pieces = (p.V + 8 * L.piece - 1) / (8 * L.piece) * 8;  // (a slice is a multiple of that)
+    L.bits = p.V <= 4 * MANY ? 2 : p.V <= 16 * MANY ? 4 : 6;
+    L.pieces = (p.V + (8 << L.bits) - 1) / (8 << L.bits) * 8;  // (a slice is a multiple of that)
     size_t off = 0;
     auto take = [&](size_t n) {
         char *at = ws ? ws + off : nullptr;
