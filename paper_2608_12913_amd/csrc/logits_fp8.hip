@@ -37,8 +37,8 @@ struct StreamGeo {
     static_assert(SLOTS > TB && (KS == 1 ? 2 : 1) * LDS <= 160 * 1024, "ring");
 };
 
-// The weight stream: up to 64 rows, bound by HBM: 82 us for one row and 96 us for 64 rows of
-// 128,256 tokens at d = 4096 (6.4 and 5.8 TB/s; each wave reading its matrix operands
+// The weight stream: up to 64 rows, bound by HBM: 82 to 85 us for one row and 96 to 98 us for 64
+// rows of 128,256 tokens at d = 4096 (6.3 and 5.8 TB/s; each wave reading its matrix operands
 // straight from memory took 116 and 339 us).  A wave owns 16 TB tokens x 16 RB rows.
 // Weights go straight into LDS (8 rows x 128 bytes per instruction, the shape that streams
 // fastest), into a ring of the wave's own: a slot is filled again as soon as its tile has

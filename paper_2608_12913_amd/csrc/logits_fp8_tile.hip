@@ -20,8 +20,8 @@
 // norm on normally distributed data): a hundredth of the rounding to bf16 that follows, and the
 // reason why fp32 logits do not take it.
 //
-// What bounds it, 2048 rows of 128,256 tokens at d = 4096 in bf16: 1.08 ms, 2.0 PFLOP/s (fp32: 1.94 ms,
-// 1.1 PFLOP/s).  A library product of the same codes with one scale per matrix takes 0.95 ms.
+// What bounds it, 2048 rows of 128,256 tokens at d = 4096 in bf16: 1.04 to 1.08 ms, 2.0 PFLOP/s (fp32:
+// 1.94 ms, 1.1 PFLOP/s).  A library product of the same codes with one scale per matrix takes 0.95 ms.
 // Timing copies: without the stores 0.89 ms, without the loads as well 0.76, without the LDS reads
 // as well 0.66; the matrix cores alone need 0.48 at the clock that the card holds.  Measured and
 // not kept: deeper rings (nothing), workgroups that walk several tiles and ask for the next one's
