@@ -1233,7 +1233,8 @@ __global__ __launch_bounds__(ST) void spread_kernel(SampleProblem P, Scan L) {
     const int per = (P.V + SLICE - 1) / SLICE, r = blockIdx.x / per, s = blockIdx.x % per, tid = threadIdx.x;
     const Spread spread = L.spread[r];
     const Rules rules(P, r);
-    if (!rules.whole && spread.least > spread.top) return;
+    const bool none = spread.least == 0xffffffffu;  // (which is the key of a NaN)
+    if (!rules.whole && (none || spread.least > spread.top)) return;
     const char *row = row_of<DT>(P, r);
     f32x4 z[SLICE / ST / 4];
 #pragma unroll
@@ -1250,7 +1251,7 @@ __global__ __launch_bounds__(ST) void spread_kernel(SampleProblem P, Scan L) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const uint32_t key = key_of(z[i][j]);
-            in[j] = key >= spread.least;
+            in[j] = !none && key >= spread.least;
             q[j] = in[j] ? (float)(W.exact(key) * spread.scale) : 0.f;
         }
         if (rules.whole && e + 3 < P.V) {

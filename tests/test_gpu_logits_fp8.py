@@ -109,6 +109,35 @@ def test_large_vocabulary(M, dtype):
     assert bool(((out.double() - z).abs() <= tol).all())
 
 
+@pytest.mark.parametrize("M, dtype", [(2, "f32"), (70, "bf16")])
+def test_weights_and_logits_past_32_bits(M, dtype):
+    """5 GB of weights, and rows of logits 2^30 elements apart (the last ones past 2^32 bytes): the last
+    tokens against the product of the decoded codes in 64 bits, as above."""
+    N, K, last, stride = 1250000, 4096, 1280, 1 << 30 if M < 10 else 1 << 26
+    gen = torch.Generator(device=DEV).manual_seed(M)
+    draw = lambda *n: torch.randint(0, 126, n, generator=gen, device=DEV, dtype=torch.uint8)  # noqa: E731
+    h, w, hs = draw(M, K), draw(N, K), torch.rand(M, K // 128, generator=gen, device=DEV)
+    ws = torch.rand(-(-N // 128), K // 128, generator=gen, device=DEV)
+    first = (N - last) // 128 * 128
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    out = torch.empty((M - 1) * stride + N, dtype=t, device=DEV).as_strided((M, N), (stride, 1))
+    dcd.logits_fp8(dcd.make_fp8_problem(M, N, K, dtype, stride), dcd.make_fp8_inputs(h, hs, w, ws), out,
+                   torch.cuda.current_stream())
+    table = torch.from_numpy(oracle.decode(np.arange(256, dtype=np.uint8))).to(DEV)
+    z, mag = torch.zeros(M, N - first, device=DEV, dtype=torch.float64), 0
+    for b in range(K // 128):
+        s = slice(128 * b, 128 * b + 128)
+        hv = table[h[:, s].int()] * hs[:, b, None].double()
+        wv = (table[w[first:, s].int()] * ws[first // 128:, b].double().repeat_interleave(128)[:N - first, None]).t().contiguous()
+        z += hv @ wv
+        mag = mag + hv.abs() @ wv.abs()
+    tol = (130 + K // 128) * 2.0 ** -23 * mag
+    if dtype == "bf16":
+        tol = tol + 7 * 2.0 ** -13 * mag
+        tol = tol + 2.0 ** -8 * (z.abs() + tol)
+    assert bool(((out[:, first:].double() - z).abs() <= tol).all())
+
+
 def test_exact_integers():
     """Small integers and scales of one: every sum is exact, so the logits are too."""
     rng = np.random.RandomState(1)

@@ -192,6 +192,19 @@ def test_rules_outside_their_range_leave_the_row_without_a_token():
         assert c.results()[0].tolist()[1:11] == [-1] * 10 and c.results()[0][0] >= 0 and c.results()[0][11] >= 0
 
 
+@pytest.mark.parametrize("V", [2, 700, 9001, 40000])
+@pytest.mark.parametrize("bits", [0x7fffffff, -1, 0x7f800001])
+def test_every_kind_of_nan_leaves_the_row_without_a_token(V, bits):
+    """NaN of any payload and sign, with rules of each kind and without."""
+    z = logits(8, V, 19)
+    z.view(np.int32)[::2, V // 2] = np.int32(bits)
+    off = dict(top_k=np.zeros(8, np.int32), top_p=np.ones(8, np.float32), min_p=np.zeros(8, np.float32))
+    for name, value in (("top_k", 5), ("top_p", 0.7), ("min_p", 0.1), ("top_p", 1.0)):
+        rules = {n: a.copy() for n, a in off.items()}
+        rules[name][:] = value
+        Call(z, uniforms(8, 20), **rules).run().check()
+
+
 @pytest.mark.parametrize("V", [900, 30011])
 def test_first_and_last_uniforms(V):
     z = logits(8, V, 11, 1.0)
@@ -199,6 +212,23 @@ def test_first_and_last_uniforms(V):
     u = np.array([0.0, 1 - 2.0 ** -24, 0.0, 1 - 2.0 ** -24] * 2)
     k = np.array([0, 0, 30, 30] * 2, np.int32)
     Call(z, u, top_k=k).run().check()
+
+
+@pytest.mark.parametrize("V", [(1 << 20) - 3, 1 << 20, (1 << 20) + 5])
+def test_the_longest_rows(V):
+    """Either side of the longest vocabulary that is read in slices."""
+    R = 9
+    z = np.random.RandomState(2).randn(R, V).astype(np.float32) * 4
+    rules = mixed(R, 5)
+    rules["temperature"][0], rules["top_k"][0], rules["top_p"][0], rules["min_p"][0] = 1, 0, 1, 0
+    rules["top_k"][4] = 3000
+    Call(z, uniforms(R, 6), **rules).run().check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_past_32_bits(dtype):
+    """The third row starts 2^31 elements behind the first."""
+    Call(logits(3, 5003, 21), uniforms(3, 21), dtype, 1 << 30, **mixed(3, 22)).run().check()
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
