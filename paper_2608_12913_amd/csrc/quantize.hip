@@ -172,9 +172,12 @@ template <int DT>
 hipError_t launch(const QuantProblem &p, hipStream_t st) {
     if (p.block_rows == 1) {
         const long long ngroups = p.rows * p.groups;
-        // few groups: one each, so that they spread over the chip
+        // One group per 16 lanes, or four: for many groups of bf16, and for more fp32 ones than a launch
+        // counts threads for.  One and four, us: bf16 rows of 4,096, 512 of them 3.4 and 5.0, 2,048: 8.2 and 8.6,
+        // 4,096: 15.2 and 14.4, 16,384 of 8,192: 97 and 86; fp32, 8,192 of 4,096: 31 and 35, 65,536 of 8,192:
+        // 464 and 510.
         constexpr int UN = 4;
-        const bool many = ngroups > (long long)NT / LG * 4096;
+        const bool many = ngroups > (DT == kBF16 ? 1LL << 16 : 1LL << 27);
         const long long per = NT / LG * (many ? UN : 1);
         const dim3 grid((unsigned)((ngroups + per - 1) / per));
         if (many)
