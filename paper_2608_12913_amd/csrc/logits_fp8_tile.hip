@@ -97,13 +97,14 @@ struct Loader {
     static constexpr int L = G == 0 ? WL : Q::HL;
     Rows codes, scales;
     uint32_t off, soff, col, K;
-    int lds_codes, lds_scale, nb;
+    int lds_codes, lds_scale, nb, rot;
 
-    __device__ __forceinline__ void init(const Fp8Problem &P, int tok0, int row0, int wv) {
+    __device__ __forceinline__ void init(const Fp8Problem &P, int tok0, int row0, int wv, int start) {
         const int lane = threadIdx.x % 64;
         col = (uint32_t)(lane % 8 ^ lane / 8) * 16;
         K = (uint32_t)P.K;
         nb = P.groups;
+        rot = start;
         if constexpr (G == 0) {
             const int t0 = tok0 + WT * wv;
             codes = Rows(P.w + (size_t)t0 * K, P.N - t0, K);
@@ -119,14 +120,18 @@ struct Loader {
             lds_scale = wv * 8 * RB * SB * 4;
         }
     }
-    // Block b's stage (hidden states: part `par` of the rows) into `to`.  Past the last block: the
-    // last one again (never read).
+    // The b-th block of the walk along K; past the last one: that one again (never read).
+    __device__ __forceinline__ int block(int b) const {
+        b = min(b, nb - 1) + rot;
+        return b < nb ? b : b - nb;
+    }
+    // Block b's stage (hidden states: part `par` of the rows) into `to`.
     struct Request {
         uint32_t at;
         char *to;
     };
     __device__ __forceinline__ Request request(int b, int par, char *to) const {
-        Request r{off + min((uint32_t)min(b, nb - 1) * kGroup + col, K - 16) + (G == 0 ? 0u : (uint32_t)(par * Q::HALF) * K),
+        Request r{off + min((uint32_t)block(b) * kGroup + col, K - 16) + (G == 0 ? 0u : (uint32_t)(par * Q::HALF) * K),
                   to + lds_codes};
         asm volatile("" : "+v"(r.at));  // made here, not between the products that the loads are spread over
         return r;
@@ -141,7 +146,7 @@ struct Loader {
     }
     // scales of blocks b .. b + SB - 1 (a row's last ones run on into the next row's: not used)
     __device__ __forceinline__ void load_scales(int b, char *to) const {
-        scales.load(soff + (uint32_t)b * 4, to + lds_scale);
+        scales.load(soff + (uint32_t)block(b) * 4, to + lds_scale);
     }
 };
 
@@ -275,14 +280,14 @@ __device__ __forceinline__ void multiply(const Operands<RB / 2> &o, const Wide (
 // Requests past the end repeat the last block, so that the waits count the same loads (scales
 // only make them stricter).
 template <int RB, int G, bool FAST, int DT>
-__device__ __forceinline__ void work(const Fp8Problem &P, char *lds, int tok0, int row0, int wv) {
+__device__ __forceinline__ void work(const Fp8Problem &P, char *lds, int tok0, int row0, int wv, int start) {
     using Q = TileGeo<RB>;
     constexpr int QB = Q::QB, NW = Q::NW, NH = Q::NH;
     static_assert(NH - 2 < 2 * SB - 1, "scales have landed before they are read");
     const int lane = threadIdx.x % 64, n = lane % 16, g = lane / 16;
     char *hring = lds + NW * WSTAGE, *sring = lds + Q::SAT;
     Loader<RB, G> ld;
-    ld.init(P, tok0, row0, wv);
+    ld.init(P, tok0, row0, wv, start);
     if constexpr (G == 0) {
 #pragma unroll
         for (int c = 0; c < NW; ++c) ld.load_all(ld.request(c, 0, lds + c * WSTAGE));
@@ -304,20 +309,20 @@ __device__ __forceinline__ void work(const Fp8Problem &P, char *lds, int tok0, i
     uint32_t wcur = 0, hcur = 0, scur = 0;
     auto next = [](uint32_t x, uint32_t stage, uint32_t ring) { return x + stage == ring ? 0u : x + stage; };
     const scalar_ptr ws = (scalar_ptr)(P.ws + (size_t)(min(tok0 + WT * wv, P.N - 1) / kGroup) * P.groups);
-    float wsc = ws[0];
+    float wsc = ws[ld.block(0)];
     f32x4 acc[VB][RB] = {};
     Operands<QB> o;
     Wide wa[FAST ? 1 : VB];
     Pending pend = {};
     if constexpr (G == 1) slot_end();
     for (int c = 0; c < P.groups; ++c) {
-        const int k = c * kGroup;
+        const int k = ld.block(c) * kGroup;
         const bool tail = k + kGroup > P.K;
         const uint32_t sc = s0 + scur + c % SB * 4;
         if constexpr (G == 1) {
             if (c % SB == 0 && c + SB < P.groups) ld.load_scales(c + SB, sring + (Q::SSTAGE - scur));
         }
-        const float wsn = ws[min(c + 1, P.groups - 1)];
+        const float wsn = ws[ld.block(c + 1)];
 #pragma unroll
         for (int par = 0; par < 2; ++par) {
             if (par == 0)
@@ -419,10 +424,17 @@ __device__ __forceinline__ void tile_body(const Fp8Problem &P, int nrow, char *l
     const int xcd = blockIdx.x % kXcds, at = blockIdx.x / kXcds;
     const int tok0 = (at / nrow * kXcds + xcd) * TT, row0 = at % nrow * TileGeo<RB>::TR;
     if (tok0 >= P.N) return;
+    // Where every weight is read once (one tile of rows), the walk along K starts at another block for
+    // each tile of tokens, so that the chip does not ask all HBM channels for the same columns at once
+    // (scales are loaded SB blocks at a time, so only where their number divides).  From the first
+    // block and like this, us, 100 rows in bf16, d = 2048, 4096, 6144, 8192, 16384: 65,536 tokens 37 and 34, 73 and
+    // 70, 88 and 86, 135 and 103, 195 and 186; 128,256 tokens, 4096: 141 and 143.  With more rows the weights come from
+    // the caches: 512 rows of 65,536, 8192 266 and 268, 1024 of 6144 387 and 397.
+    const int start = nrow == 1 && P.groups % SB == 0 ? (int)((unsigned)(tok0 / TT) * SB % (unsigned)P.groups) : 0;
     if (wave < 4)
-        work<RB, 0, FAST, DT>(P, lds, tok0, row0, wave);
+        work<RB, 0, FAST, DT>(P, lds, tok0, row0, wave, start);
     else
-        work<RB, 1, FAST, DT>(P, lds, tok0, row0, wave - 4);
+        work<RB, 1, FAST, DT>(P, lds, tok0, row0, wave - 4, start);
 }
 
 template <int RB, bool FAST, int DT>

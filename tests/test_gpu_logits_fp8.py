@@ -72,6 +72,13 @@ def test_sizes(M, N, K, dtype):
     _check(M, N, K, dtype)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M, N, K", [(70, 1500, 2000), (100, 2050, 976), (128, 5000, 1024), (190, 3000, 8176), (66, 9000, 1600)])
+def test_one_tile_of_rows(M, N, K, dtype):
+    """Each tile of tokens walks K from a block of its own, and a short last block comes in between."""
+    _check(M, N, K, dtype)
+
+
 @pytest.mark.parametrize("M", [1, 16, 64, 150])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_strides_and_no_bias(M, dtype):
