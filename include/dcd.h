@@ -370,8 +370,10 @@ typedef struct {               /* device pointers, written by the call          
  * over the top_k; of those the ones with w >= min_p (of the largest probability).  At
  * least one token is kept, -inf never.  The token is drawn from the kept weights by inverse
  * CDF in token-id order: the smallest token whose cumulative weight exceeds u times the
- * total.  probs is w over that total, 0 for what was not kept.  Weights and their sums are
- * held in 64 bits.
+ * total.  probs is w over that total, 0 for what was not kept.  Weights are held in 64 bits,
+ * their sums as 64-bit whole numbers of steps of the largest weight times V 2^-62 (V rounded up
+ * to a power of two of at least 4,096), the same in every call: a token under half a step is kept,
+ * but not drawn.
  * A row with a NaN or +inf logit, with no finite logit, or with a rule or uniform outside
  * its range gets token -1, kept 0, logprob NaN and probs 0.
  * Workspace: device memory of at least dcd_sample_workspace_bytes(p), 256-byte aligned, not

@@ -11,7 +11,7 @@ constexpr size_t kAlign = 256;
 constexpr long long kMaxRows = 1 << 24;
 constexpr long long kMaxVocab = 1 << 30;
 constexpr int kMaxHidden = 1 << 20;
-// a launch counts its threads in 32 bits: workgroups of 256 threads take 64 row groups or one block
+// a launch counts its threads in 32 bits: workgroups of 256 threads take up to 64 row groups, or one block
 constexpr long long kMaxRowGroups = (1LL << 30) - 64;
 constexpr long long kMaxBlocks = (1LL << 24) - 1;
 
@@ -104,7 +104,7 @@ int make_sample(const dcd_sample_problem *p, SampleProblem &P) {
     const int64_t stride = p->stride ? p->stride : p->vocab;
     if (stride < p->vocab || stride > kMaxVocab) return DCD_ERR_SHAPE;
     if (!logit_type(p->dtype)) return DCD_ERR_PARAM;
-    // a launch counts its threads in 32 bits: 1024 per row, 256 per slice of at least 2,048 tokens
+    // a launch counts its threads in 32 bits: 512 per row, 256 per slice of at least 2,048 tokens
     if (p->rows >= 1 << 22 || ((int64_t)p->vocab / 2048 + 1) * p->rows >= 1 << 24) return DCD_ERR_SHAPE;
     P = SampleProblem{};
     P.R = p->rows;
