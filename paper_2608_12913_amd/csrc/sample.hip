@@ -26,12 +26,12 @@
 // What bounds it, rows of 128,256 fp32 logits without dense probabilities, us (of which a streaming
 // read needs 0.1, 10 and 77):
 //                         1 row   128 rows   1,024 rows
-//   argmax                 19.6     33         130
-//   top-k 50               20.3     34         134    memory, and 20 us of a row's dependent steps
-//   min-p 0.05             22.2     40         161
-//   no rule                12.2     41         207    a 64-bit exponential per logit
-//   top-p 0.9              31.5     58         244    the same, and the slices' histograms
-//   top-p 0.9, flat        105      132        443    a bracket of thousands: order, second reading
+//   argmax                 19.4     33         130
+//   top-k 50               20.4     34         132    memory, and 20 us of a row's dependent steps
+//   min-p 0.05             22.5     41         159
+//   no rule                11.9     41         198    a 64-bit exponential per logit
+//   top-p 0.9              31.3     58         235    the same, and the slices' histograms
+//   top-p 0.9, flat        104      130        430    a bracket of thousands: order, second reading
 // A row by one workgroup from the logits alone, with a radix search of all of them per level, took
 // 301 us (1 row, top-k and top-p) and 2,156 us (1,024 rows of mixed rules, 345 now).
 #include "proposal.h"
@@ -92,9 +92,8 @@ struct Weights {
     const double *table;
     __device__ __forceinline__ Weights(uint32_t top_key, float T, int shift, const double *table_)
         : top((double)logit_of(top_key)), per(1.0 / kLn / (double)T), one((double)(1ull << shift)), table(table_) {}
-    __device__ __forceinline__ double exact(uint32_t key) const {
-        return power_of(((double)logit_of(key) - top) * per, table);
-    }
+    __device__ __forceinline__ double of(float z) const { return power_of(((double)z - top) * per, table); }
+    __device__ __forceinline__ double exact(uint32_t key) const { return of(logit_of(key)); }
     __device__ __forceinline__ u64 to_fixed(double w) const {  // w <= 1: rounded by the sum with 2^52
         return (u64)__double_as_longlong(fma(w, one, 0x1p52)) - 0x4330000000000000ull;
     }
@@ -618,10 +617,9 @@ __global__ __launch_bounds__(ST) void scan_kernel(SampleProblem P, Scan L) {
         for (int i = 0; i < EPT / 4; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const uint32_t key = key_of(z[i][j]);
                 const float bin = first - bin_of(z[i][j], per);
-                if (key < kLowest || bin >= most) continue;
-                const u64 w = W.fixed(key);
+                if (z[i][j] == -INFINITY || bin >= most) continue;
+                const u64 w = W.to_fixed(W.of(z[i][j]));
                 m += w;
                 if (!rules.whole && w && bin < HB - 1.f) atomicAdd(&hist[(int)bin], w);
             }
@@ -1233,8 +1231,7 @@ __global__ __launch_bounds__(ST) void spread_kernel(SampleProblem P, Scan L) {
     const int per = (P.V + SLICE - 1) / SLICE, r = blockIdx.x / per, s = blockIdx.x % per, tid = threadIdx.x;
     const Spread spread = L.spread[r];
     const Rules rules(P, r);
-    const bool none = spread.least == 0xffffffffu;  // (which is the key of a NaN)
-    if (!rules.whole && (none || spread.least > spread.top)) return;
+    if (!rules.whole && (spread.least == 0xffffffffu || spread.least > spread.top)) return;
     const char *row = row_of<DT>(P, r);
     f32x4 z[SLICE / ST / 4];
 #pragma unroll
@@ -1242,6 +1239,7 @@ __global__ __launch_bounds__(ST) void spread_kernel(SampleProblem P, Scan L) {
     fill_table(table);
     __syncthreads();
     const Weights W(spread.top, rules.T, 0, table);
+    const float least = logit_of(spread.least);  // (none: a NaN)
     float *probs = P.probs + (size_t)r * P.V;
 #pragma unroll
     for (int i = 0; i < SLICE / ST / 4; ++i) {
@@ -1250,9 +1248,8 @@ __global__ __launch_bounds__(ST) void spread_kernel(SampleProblem P, Scan L) {
         bool in[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const uint32_t key = key_of(z[i][j]);
-            in[j] = !none && key >= spread.least;
-            q[j] = in[j] ? (float)(W.exact(key) * spread.scale) : 0.f;
+            in[j] = z[i][j] >= least;
+            q[j] = in[j] ? (float)(W.of(z[i][j]) * spread.scale) : 0.f;
         }
         if (rules.whole && e + 3 < P.V) {
             __builtin_nontemporal_store(q, reinterpret_cast<f32x4_any *>(probs + e));
