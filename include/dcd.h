@@ -331,10 +331,9 @@ typedef struct {               /* device pointers, read only                    
  * Logits of a head held in 8 bits:
  *   z[r, v] = sum over blocks b of 128 columns of
  *               h_scale[r, b] * w_scale[v / 128, b] * sum_{k in b} h[r, k] w[v, k]  + bias[v]
- * with exact products, fp32 sums, and one rounding at the end for bf16 logits.  bf16 logits
- * of more than 64 rows are multiplied by the 8-bit matrix instructions, which align the
- * products of eight consecutive columns to the largest of them: they may be off by 7 * 2^-13 of
- * the sum of the products' magnitudes (typically 1e-5 of the logit) before that rounding.
+ * with exact products and fp32 sums; bf16 logits are the fp32 ones, rounded once.  The order in
+ * which the blocks are added depends on the problem's sizes, so a row's logits may differ in their
+ * last bits with the number of rows in the call.
  * Elements of `logits` between V and the row stride are left as they were.  Needs no
  * workspace.
  */

@@ -3,8 +3,9 @@
 // with e4m3 codes and fp32 scales per 128 columns (and, of the weights, 128 tokens).
 //
 // Up to 64 rows here, more in logits_fp8_tile.hip.  The codes are widened to bf16 in registers
-// (exactly) and multiplied there: the weight stream leaves the matrix cores the time, and their
-// 8-bit instructions lose bits (there).
+// (exactly) and multiplied there, with sums in fp32; the matrix cores' 8-bit instructions lose bits
+// (there).  Both files take a block's product alike, and the type of the logits changes nothing
+// but the last rounding; the order of the blocks depends on the number of rows.
 //
 // A = weights (tokens), B = hidden states (rows), so a lane's four results belong to one row
 // and the block's scale is one number per lane and row block.  Each block's product starts

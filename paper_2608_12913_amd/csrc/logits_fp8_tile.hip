@@ -13,21 +13,18 @@
 // slot behind the first, so that one wave of a SIMD multiplies while the other reads.  Every
 // slot ends with a workgroup barrier.
 //
-// fp32 logits: the codes are widened to bf16 in registers, which is exact.  bf16 logits:
-// v_mfma_f32_16x16x128_f8f6f4 multiplies the codes themselves at twice the rate.  It aligns the
-// eight products of a group of columns before it adds them and drops what lies 13 bits below the
-// largest one's power of two (measured: at most 5 of the 7 possible units, 1.3e-5 of the logits'
-// norm on normally distributed data): a hundredth of the rounding to bf16 that follows, and the
-// reason why fp32 logits do not take it.
+// The codes are widened to bf16 in registers, which is exact, and multiplied there, for logits of
+// either type.  v_mfma_f32_16x16x128_f8f6f4 would multiply the codes themselves at twice the rate
+// (2048 rows: 1.06 ms), but it aligns the eight products of a group of columns before it adds them
+// and drops what lies 13 bits below the largest one's power of two (measured: at most 5 of the 7
+// possible units): where large products cancel, a logit is lost in that.
 //
-// What bounds it, 2048 rows of 128,256 tokens at d = 4096 in bf16: 1.04 to 1.08 ms, 2.0 PFLOP/s (fp32:
-// 1.94 ms, 1.1 PFLOP/s).  A library product of the same codes with one scale per matrix takes 0.95 ms.
-// Timing copies: without the stores 0.89 ms, without the loads as well 0.76, without the LDS reads
-// as well 0.66; the matrix cores alone need 0.48 at the clock that the card holds.  Measured and
-// not kept: deeper rings (nothing), workgroups that walk several tiles and ask for the next one's
-// stages ahead (+10%: the choice of the tile costs more between the products than the wait it
-// saves), workgroups set apart in time (-2%), non-temporal stores (+2%), stores straight from the
-// registers (+3%, ragged rows +9%).
+// What bounds it, 2048 rows of 128,256 tokens at d = 4096: 1.79 ms in bf16 (fp32: 1.81), 1.2 PFLOP/s.
+// Timing copies: without the widening 1.44 ms, without the stores 1.69.  Measured with the 8-bit
+// instruction's shorter products, and not kept: deeper rings (nothing), workgroups that walk several
+// tiles and ask for the next one's stages ahead (+10%: the choice of the tile costs more between the
+// products than the wait it saves), workgroups set apart in time (-2%), non-temporal stores (+2%), stores
+// straight from the registers (+3%, ragged rows +9%).
 #include "logits_fp8.h"
 
 namespace dcd {
@@ -53,10 +50,8 @@ struct TileGeo {
     static constexpr int SAT = NW * WSTAGE + NH * HSTAGE;
     static constexpr int BAT = SAT + 2 * SSTAGE;   // bias of the tokens
     static constexpr int LDS = BAT + TT * 4;
-    static_assert(RB % 2 == 0 && RB <= 8, "tile");
+    static_assert(RB == 4 || RB == 6, "operands of two or three row blocks");
 };
-
-typedef __attribute__((ext_vector_type(8))) int i32x8;
 
 // The token (of a wave's 64) at row r of its tiles in LDS.  Block v = 16 rows, and a lane's results
 // are rows 4 g .. 4 g + 3 of each: this way those of two blocks are 8 tokens in a row, and the four
@@ -157,14 +152,12 @@ struct Loader {
 #define DCD_RB1 DCD_RD("b0", "b1", "h", "0") "ds_read_b32 %[s0], %[s]\n "
 #define DCD_RB2 DCD_RB1 DCD_RD("b2", "b3", "h", "2048") "ds_read_b32 %[s1], %[s] offset:256\n "
 #define DCD_RB3 DCD_RB2 DCD_RD("b4", "b5", "h", "4096") "ds_read_b32 %[s2], %[s] offset:512\n "
-#define DCD_RB4 DCD_RB3 DCD_RD("b6", "b7", "h", "6144") "ds_read_b32 %[s3], %[s] offset:768\n "
 #define DCD_OA                                                                                          \
     [a0] "=&v"(a[0]), [a1] "=&v"(a[1]), [a2] "=&v"(a[2]), [a3] "=&v"(a[3]), [a4] "=&v"(a[4]),          \
         [a5] "=&v"(a[5]), [a6] "=&v"(a[6]), [a7] "=&v"(a[7])
 #define DCD_OB1 [b0] "=&v"(b[0]), [b1] "=&v"(b[1]), [s0] "=&v"(s[0])
 #define DCD_OB2 DCD_OB1, [b2] "=&v"(b[2]), [b3] "=&v"(b[3]), [s1] "=&v"(s[1])
 #define DCD_OB3 DCD_OB2, [b4] "=&v"(b[4]), [b5] "=&v"(b[5]), [s2] "=&v"(s[2])
-#define DCD_OB4 DCD_OB3, [b6] "=&v"(b[6]), [b7] "=&v"(b[7]), [s3] "=&v"(s[3])
 #define DCD_IB [h] "v"(h), [hx] "v"(h ^ 64u), [s] "v"(sc)
 #define DCD_READ_ALL(n)                                                                       \
     asm volatile(DCD_RA DCD_RB##n "s_waitcnt lgkmcnt(0)"                                      \
@@ -180,16 +173,12 @@ struct Operands {
     float s[QB];
 
     __device__ __forceinline__ void read_all(uint32_t w, uint32_t h, uint32_t sc) {
-        if constexpr (QB == 1) DCD_READ_ALL(1);
         if constexpr (QB == 2) DCD_READ_ALL(2);
         if constexpr (QB == 3) DCD_READ_ALL(3);
-        if constexpr (QB == 4) DCD_READ_ALL(4);
     }
     __device__ __forceinline__ void read_rows(uint32_t h, uint32_t sc) {
-        if constexpr (QB == 1) DCD_READ_ROWS(1);
         if constexpr (QB == 2) DCD_READ_ROWS(2);
         if constexpr (QB == 3) DCD_READ_ROWS(3);
-        if constexpr (QB == 4) DCD_READ_ROWS(4);
     }
     // columns past the end of the rows count as zero
     __device__ __forceinline__ void zero_tail(int k, int K) {
@@ -202,10 +191,6 @@ struct Operands {
     }
 };
 
-__device__ __forceinline__ i32x8 join(const u32x4 &x, const u32x4 &y) {
-    return i32x8{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
-}
-
 // Products whose results are not added yet: a product's result is there two products later, so
 // the matrix cores never wait for the additions.
 struct Pending {
@@ -215,8 +200,8 @@ struct Pending {
 
 // One stage's products, added to row blocks R0 .. of the sums (and the last two of the stage
 // before to row block RP), with the loads LO .. HI-1 of a stage spread over them.
-template <int RB, int R0, int RP, bool FAST, class L>
-__device__ __forceinline__ void multiply(const Operands<RB / 2> &o, const Wide (&wa)[FAST ? 1 : VB], float ws,
+template <int RB, int R0, int RP, class L>
+__device__ __forceinline__ void multiply(const Operands<RB / 2> &o, const Wide (&wa)[VB], float ws,
                                          Pending &pend, f32x4 (&acc)[VB][RB], const L &ld, const typename L::Request &req,
                                          int lo, int hi) {
     constexpr int QB = RB / 2, N = VB * QB;
@@ -224,28 +209,19 @@ __device__ __forceinline__ void multiply(const Operands<RB / 2> &o, const Wide (
     p[1] = pend.p[0];
     p[2] = pend.p[1];
     float s = 0.f, before = pend.s;
-    Wide x[FAST ? 1 : 2];
-    i32x8 xb;
-    if constexpr (!FAST) x[0].set(o.b[0], o.b[1]);
+    Wide x[2];
+    x[0].set(o.b[0], o.b[1]);
     __builtin_amdgcn_s_setprio(1);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int k = 0; k < N; ++k) {
         const int j = k / VB, v = k % VB;
-        if (v == 0) {
-            s = o.s[j] * ws;
-            if constexpr (FAST) xb = join(o.b[2 * j], o.b[2 * j + 1]);
-        }
+        if (v == 0) s = o.s[j] * ws;
 #pragma unroll
         for (int q = 0; q < 16; ++q)
             if (q >= lo && q < hi && (q - lo) * N / (hi > lo ? hi - lo : 1) == k) ld.load(req, q);
-        if constexpr (FAST) {
-            p[k % 3] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(join(o.a[2 * v], o.a[2 * v + 1]), xb,
-                                                                        f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
-        } else {
-            if (v == 1 && j + 1 < QB) x[(j + 1) % 2].set(o.b[2 * j + 2], o.b[2 * j + 3]);
-            p[k % 3] = product(wa[v], x[j % 2]);
-        }
+        if (v == 1 && j + 1 < QB) x[(j + 1) % 2].set(o.b[2 * j + 2], o.b[2 * j + 3]);
+        p[k % 3] = product(wa[v], x[j % 2]);
         const int k2 = k - 2, row = k2 < 0 ? RP : R0 + k2 / VB, v2 = (k2 + VB) % VB;
         const float s2 = k2 < 0 || k2 / VB < j ? before : s;
 #pragma unroll
@@ -279,7 +255,7 @@ __device__ __forceinline__ void multiply(const Operands<RB / 2> &o, const Wide (
 //     first block of every SB for the scales of the SB blocks after these.
 // Requests past the end repeat the last block, so that the waits count the same loads (scales
 // only make them stricter).
-template <int RB, int G, bool FAST, int DT>
+template <int RB, int G, int DT>
 __device__ __forceinline__ void work(const Fp8Problem &P, char *lds, int tok0, int row0, int wv, int start) {
     using Q = TileGeo<RB>;
     constexpr int QB = Q::QB, NW = Q::NW, NH = Q::NH;
@@ -312,7 +288,7 @@ __device__ __forceinline__ void work(const Fp8Problem &P, char *lds, int tok0, i
     float wsc = ws[ld.block(0)];
     f32x4 acc[VB][RB] = {};
     Operands<QB> o;
-    Wide wa[FAST ? 1 : VB];
+    Wide wa[VB];
     Pending pend = {};
     if constexpr (G == 1) slot_end();
     for (int c = 0; c < P.groups; ++c) {
@@ -330,11 +306,9 @@ __device__ __forceinline__ void work(const Fp8Problem &P, char *lds, int tok0, i
             else
                 o.read_rows(h0 + hcur, sc + QB * 16 * SB * 4);
             if (tail) o.zero_tail(k, P.K);
-            if constexpr (!FAST) {
-                if (par == 0) {
+            if (par == 0) {
 #pragma unroll
-                    for (int v = 0; v < VB; ++v) wa[v].set(o.a[2 * v], o.a[2 * v + 1]);
-                }
+                for (int v = 0; v < VB; ++v) wa[v].set(o.a[2 * v], o.a[2 * v + 1]);
             }
             if constexpr (G == 1) wait_loads<(NH - 2) * Q::HL>();
             // G = 1: stage 2 c + par + NH
@@ -349,9 +323,9 @@ __device__ __forceinline__ void work(const Fp8Problem &P, char *lds, int tok0, i
             slot_end();
             constexpr int LO = G == 0 ? WL / 2 : 0, HI = G == 0 ? WL : Q::HL;
             if (par == 0)
-                multiply<RB, 0, RB - 1, FAST>(o, wa, wsc, pend, acc, ld, req, G == 0 ? HI : LO, HI);
+                multiply<RB, 0, RB - 1>(o, wa, wsc, pend, acc, ld, req, G == 0 ? HI : LO, HI);
             else
-                multiply<RB, QB, QB - 1, FAST>(o, wa, wsc, pend, acc, ld, req, LO, HI);
+                multiply<RB, QB, QB - 1>(o, wa, wsc, pend, acc, ld, req, LO, HI);
             if constexpr (G == 0) {
                 if (par == 1) wait_loads<(NW - 1) * WL>();
             }
@@ -416,7 +390,7 @@ __device__ __forceinline__ void work(const Fp8Problem &P, char *lds, int tok0, i
     }
 }
 
-template <int RB, bool FAST, int DT>
+template <int RB, int DT>
 __device__ __forceinline__ void tile_body(const Fp8Problem &P, int nrow, char *lds) {
     int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     asm("" : "+s"(wave));
@@ -427,53 +401,43 @@ __device__ __forceinline__ void tile_body(const Fp8Problem &P, int nrow, char *l
     // Where every weight is read once (one tile of rows), the walk along K starts at another block for
     // each tile of tokens, so that the chip does not ask all HBM channels for the same columns at once
     // (scales are loaded SB blocks at a time, so only where their number divides).  From the first
-    // block and like this, us, 100 rows in bf16, d = 2048, 4096, 6144, 8192, 16384: 65,536 tokens 37 and 34, 73 and
-    // 70, 88 and 86, 135 and 103, 195 and 186; 128,256 tokens, 4096: 141 and 143.  With more rows the weights come from
-    // the caches: 512 rows of 65,536, 8192 266 and 268, 1024 of 6144 387 and 397.
+    // block and like this, us, 100 rows in bf16, d = 2048, 4096, 6144, 8192, 16384: 65,536 tokens 42 and 42, 76 and
+    // 71, 105 and 102, 142 and 133, 256 and 252; 128,256 tokens, 4096: 150 and 140.  With more rows the weights come
+    // from the caches: 512 rows of 65,536, 8192 467 and 487, 1024 of 6144 685 and 721.
     const int start = nrow == 1 && P.groups % SB == 0 ? (int)((unsigned)(tok0 / TT) * SB % (unsigned)P.groups) : 0;
     if (wave < 4)
-        work<RB, 0, FAST, DT>(P, lds, tok0, row0, wave, start);
+        work<RB, 0, DT>(P, lds, tok0, row0, wave, start);
     else
-        work<RB, 1, FAST, DT>(P, lds, tok0, row0, wave - 4, start);
+        work<RB, 1, DT>(P, lds, tok0, row0, wave - 4, start);
 }
 
-template <int RB, bool FAST, int DT>
+template <int RB, int DT>
 __global__ __launch_bounds__(512, 2) void logits_tile_kernel(Fp8Problem P, int nrow) {
     __shared__ __align__(128) char lds[TileGeo<RB>::LDS];
-    tile_body<RB, FAST, DT>(P, nrow, lds);
+    tile_body<RB, DT>(P, nrow, lds);
 }
 
-template <int RB, bool FAST, int DT>
+template <int RB, int DT>
 hipError_t launch(const Fp8Problem &p, hipStream_t st) {
     const int nrow = (p.M + 32 * RB - 1) / (32 * RB), ntok = ((p.N + TT - 1) / TT + kXcds - 1) / kXcds * kXcds;
-    hipLaunchKernelGGL((logits_tile_kernel<RB, FAST, DT>), dim3((unsigned)(ntok * nrow)), dim3(512), 0, st, p, nrow);
+    hipLaunchKernelGGL((logits_tile_kernel<RB, DT>), dim3((unsigned)(ntok * nrow)), dim3(512), 0, st, p, nrow);
     return hipGetLastError();
 }
 
 }  // namespace
 
 // Row blocks per wave: the shape of the least time, taken as rounds of one workgroup per CU times a
-// round's time, which grows as 5 + 2 RB (bf16) or 5 + 4 RB (fp32).  Measured (us), RB = 4 / 6 / 8 in
-// bf16: 2048 rows of 128,256 tokens, d = 4096: 1353 / 1195 / 1078;  320 rows: 264 / 232 / 264;  160: 184 /
-// 153 / 160;  96: 143 / 148 / 154;  512 rows of 32,003 tokens, d = 2048: 53 / 63 / 43;  160: 26 / 31 / 35.
-// RB = 4 / 6 in fp32: 2048 rows of 128,256 tokens: 2035 / 1938;  256: 285 / 347;  160: 261 / 193.
+// round's time, which grows as 5 + 4 RB.  Measured (us), RB = 4 / 6 in bf16 (fp32 within 5%), d = 4096: 2048 rows
+// of 128,256 tokens: 1860 / 1796;  320: 350 / 333;  256: 254 / 322;  160: 235 / 176;  96: 140 / 168;  of 32,003
+// tokens, d = 2048: 512 rows 69 / 88;  285: 68 / 48;  160: 35 / 44.  (8 does not fit the registers.)
 hipError_t launch_logits_tile(const Fp8Problem &p, hipStream_t st) {
-    const bool bf16 = p.dtype == kBF16;
-    int rb = 4;
-    long long least = 0;
-    for (int r = 4; r <= (bf16 ? 8 : 6); r += 2) {
-        const long long tiles = ((long long)p.N + TT - 1) / TT * ((p.M + 32 * r - 1) / (32 * r));
-        const long long time = (tiles + kCus - 1) / kCus * (5 + (bf16 ? 2 : 4) * r);
-        if (r == 4 || time < least) {
-            rb = r;
-            least = time;
-        }
-    }
-    if (bf16) {
-        if (rb == 4) return launch<4, true, kBF16>(p, st);
-        return rb == 6 ? launch<6, true, kBF16>(p, st) : launch<8, true, kBF16>(p, st);
-    }
-    return rb == 4 ? launch<4, false, kF32>(p, st) : launch<6, false, kF32>(p, st);
+    auto time = [&](int rb) {
+        const long long tiles = ((long long)p.N + TT - 1) / TT * ((p.M + 32 * rb - 1) / (32 * rb));
+        return (tiles + kCus - 1) / kCus * (5 + 4 * rb);
+    };
+    const bool large = time(6) < time(4), bf16 = p.dtype == kBF16;
+    if (large) return bf16 ? launch<6, kBF16>(p, st) : launch<6, kF32>(p, st);
+    return bf16 ? launch<4, kBF16>(p, st) : launch<4, kF32>(p, st);
 }
 
 }  // namespace dcd
