@@ -381,7 +381,8 @@ typedef struct {               /* device pointers, written by the call          
 int dcd_sample(const dcd_sample_problem *p, const dcd_sample_inputs *in, const dcd_sample_outputs *out,
                void *workspace, size_t workspace_bytes, void *hip_stream);
 
-/* bytes of device workspace a call with problem `p` needs (0 if `p` is invalid) */
+/* bytes of device workspace a call with problem `p` needs (0 if `p` is invalid); for one vocabulary
+   it never falls as the rows grow, so a workspace for the most rows does for fewer */
 size_t dcd_sample_workspace_bytes(const dcd_sample_problem *p);
 
 /* static description of a return code (never NULL) */

@@ -1271,10 +1271,12 @@ int bits_of(uint32_t x) {
 // 2,048, us, no rule / min-p / top-p: 1 row of 128,256 21 and 12 / 26 and 23 / 34 and 32; 24 rows 23 and 16 /
 // 27 and 26 / 39 and 39; 64 rows 29 and 25 / 31 and 34 / 42 and 47; 128 rows of 32,003 23 and 18 / 27 and 25 /
 // 35 and 33.
+int most_rows_of_short_slices(int V) { return 2 * kCus / ((V + SLICE - 1) / SLICE); }
+static_assert(MAXV <= 2048 * MAXSLICES, "short slices of the longest row");
+
 Scan layout(const SampleProblem &p, char *ws, size_t &bytes) {
     Scan L{};
-    const int large = (p.V + SLICE - 1) / SLICE;
-    L.slice = (long long)p.R * large <= 2 * kCus && p.V <= 2048 * MAXSLICES ? 2048 : SLICE;
+    L.slice = p.R <= most_rows_of_short_slices(p.V) ? 2048 : SLICE;
     L.slices = (p.V + L.slice - 1) / L.slice;
     L.bits = p.V <= 4 * MANY ? 2 : p.V <= 16 * MANY ? 4 : 6;
     L.pieces = (p.V + (8 << L.bits) - 1) / (8 << L.bits) * 8;  // (a slice is a multiple of that)
@@ -1321,9 +1323,14 @@ hipError_t launch(const SampleProblem &p, char *ws, hipStream_t st) {
 
 size_t sample_workspace(const SampleProblem &p) {
     if (p.V > MAXV || p.V < 4) return 256;
-    size_t bytes;
+    // Short slices need more per row, so that fewer rows can need more: what any number of rows up to
+    // this one needs.
+    SampleProblem fewer = p;
+    fewer.R = min(p.R, most_rows_of_short_slices(p.V));
+    size_t bytes, most;
     layout(p, nullptr, bytes);
-    return bytes;
+    layout(fewer, nullptr, most);
+    return max(bytes, most);
 }
 
 hipError_t launch_sample(const SampleProblem &p, void *ws, hipStream_t st) {
