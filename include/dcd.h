@@ -369,10 +369,12 @@ typedef struct {               /* device pointers, written by the call          
  * over the top_k; of those the ones with w >= min_p (of the largest probability).  At
  * least one token is kept, -inf never.  The token is drawn from the kept weights by inverse
  * CDF in token-id order: the smallest token whose cumulative weight exceeds u times the
- * total.  probs is w over that total, 0 for what was not kept.  Weights are held in 64 bits,
- * their sums as 64-bit whole numbers of steps of the largest weight times V 2^-62 (V rounded up
- * to a power of two of at least 4,096), the same in every call: a token under half a step is kept,
- * but not drawn.
+ * total.  probs is w over that total, 0 for what was not kept.  Weights are held in 64 bits and
+ * summed as 64-bit whole numbers of steps; a step is the largest weight times V 2^-62 (V rounded up
+ * to a power of two of at least 4,096).  A token under half a step is kept, but weighs nothing in
+ * these sums and is never drawn.  A sum may be off by about half a step per token (2^-29 of the
+ * largest weight at 128,256 tokens), which can move a draw between two tokens whose border u comes that
+ * near; how far can depend on the number of rows.  The same call gives the same bits.
  * A row with a NaN or +inf logit, with no finite logit, or with a rule or uniform outside
  * its range gets token -1, kept 0, logprob NaN and probs 0.
  * Workspace: device memory of at least dcd_sample_workspace_bytes(p), 256-byte aligned, not

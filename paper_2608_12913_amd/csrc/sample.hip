@@ -11,7 +11,9 @@
 // Sums of weights are unsigned 64-bit fixed-point numbers, at a step small enough for the vocabulary
 // (2^-45 of the largest weight at 128,256 tokens), of weights computed in 64 bits: they add
 // up to the same whatever the order, so that sums in LDS atomics give the same bits in every
-// call and a border between two tokens is where 64-bit arithmetic puts it.
+// call.  A token under half a step weighs nothing and is never drawn.  Slices of tokens are rounded as a
+// whole where they are summed before the largest weight is known, which moves a sum by about half a
+// step per token (2^-29 of the largest weight at 128,256 tokens).
 //
 // Two launches, or three.  scan_kernel reads the logits once, in slices of 2,048 or 8,192 spread over
 // the chip: the largest logit of every 64 (of fewer in short vocabularies) and, where no top-k bounds
@@ -644,8 +646,7 @@ struct PickLds {
     double scale[MAXSLICES];     // a slice's largest weight
     int below[MAXSLICES];        // bins from the row's first to the slice's first
     u64 kept[MAXSLICES];         // kept weight per slice
-    u64 unit[SLICE / UNIT];      // and per unit of a slice, with the number of its last kept token + 1
-    uint32_t last[SLICE / UNIT];
+    u64 unit[SLICE / UNIT];      // and per unit of a slice
     u64 wave[2][NW];        // of BlockScan
     u64 reach[8];                // three counts of pieces' maxima for each pair of bits
     u64 at;
@@ -816,7 +817,7 @@ __device__ __forceinline__ bool pick_row(const SampleProblem &P, const Scan &L, 
         S.ntodo = S.nlist = 0;
         S.lo_bin = S.hi_bin = HB;
     }
-    if (tid < SLICE / UNIT) S.unit[tid] = S.last[tid] = 0;
+    if (tid < SLICE / UNIT) S.unit[tid] = 0;
     if (tid < 8) S.reach[tid] = 0;
     __syncthreads();
     bad = top = finite = 0;
@@ -841,7 +842,9 @@ __device__ __forceinline__ bool pick_row(const SampleProblem &P, const Scan &L, 
         for (int i = 0; i < SPT; ++i) {
             const int s = tid + i * NT;
             if (s >= L.slices) break;
-            S.scale[s] = st[i].finite ? W.exact(st[i].top) : 0.0;
+            const double w = st[i].finite ? W.exact(st[i].top) : 0.0;
+            // a slice whose largest weight is under half a step has no token to draw: it weighs nothing
+            S.scale[s] = W.to_fixed(w) ? w : 0.0;
             S.below[s] = st[i].finite ? (int)fminf(first - bin_of(logit_of(st[i].top), per), (float)HB) : HB;
             S.kept[s] = 0;
         }
@@ -1132,7 +1135,6 @@ __device__ __forceinline__ bool pick_row(const SampleProblem &P, const Scan &L, 
             const int e = (int)(uint32_t)~x - e0;
             if (e < 0 || e >= L.slice) continue;
             atomicAdd(&S.unit[e / UNIT], W.fixed((uint32_t)(x >> 32)));
-            atomicMax(&S.last[e / UNIT], (uint32_t)~x + 1);
         }
     } else {
         f32x4 z = load4<DT>(row, e0 + wave * UNIT + lane * 4, P.V);
@@ -1141,60 +1143,43 @@ __device__ __forceinline__ bool pick_row(const SampleProblem &P, const Scan &L, 
             const f32x4 next = load4<DT>(row, e0 + min(i + NW, units - 1) * UNIT + lane * 4, P.V);
             const int e = e0 + i * UNIT + lane * 4;
             u64 w = 0;
-            uint32_t last = 0;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t key = key_of(z[j]);
-                w += weight(key, e + j);
-                if (key >= kLowest && key >= low && (key >= high || cut.keeps(key, e + j))) last = e + j + 1;
-            }
+            for (int j = 0; j < 4; ++j) w += weight(key_of(z[j]), e + j);
             w = wave_sum(w);
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) last = max(last, (uint32_t)__shfl_xor((int)last, o));
-            if (lane == 0) {
-                S.unit[i] = w;
-                S.last[i] = last;
-            }
+            if (lane == 0) S.unit[i] = w;
             z = next;
         }
     }
     __syncthreads();
     if (wave == 0) {
         const u64 w = lane < units ? S.unit[lane] : 0, run = wave_scan(w), whole = last_lane(run);
-        // a slice's weight was rounded apart from its tokens': the target may lie above them all
-        if (whole && target >= whole) target = whole - 1;
-        const u64 over = __ballot(run > target);
+        // (a slice that was picked weighs something, but it was rounded apart from its tokens: the target may
+        // lie above them all)
+        if (target >= whole) target = whole - 1;
+        const int u = __ffsll((long long)__ballot(run > target)) - 1;
+        target -= u ? (u64)__shfl((long long)run, u - 1) : 0;
+        const int e = e0 + u * UNIT + lane * 4;
+        const f32x4 x = load4<DT>(row, e, P.V);
+        u64 v[4], mine = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            v[j] = weight(key_of(x[j]), e + j);
+            mine += v[j];
+        }
+        u64 at = wave_scan(mine);
+        const u64 here = __ballot(at > target);
         int token = -1;
         float logit = 0.f;
-        if (over) {
-            const int u = __ffsll((long long)over) - 1;
-            target -= u ? (u64)__shfl((long long)run, u - 1) : 0;
-            const int e = e0 + u * UNIT + lane * 4;
-            const f32x4 x = load4<DT>(row, e, P.V);
-            u64 v[4], mine = 0;
+        if (lane == __ffsll((long long)here) - 1) {
+            at -= mine;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                v[j] = weight(key_of(x[j]), e + j);
-                mine += v[j];
-            }
-            u64 at = wave_scan(mine);
-            const u64 here = __ballot(at > target);
-            if (lane == __ffsll((long long)here) - 1) {
-                at -= mine;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    at += v[j];
-                    if (token < 0 && at > target) {
-                        token = e + j;
-                        logit = x[j];
-                    }
+                at += v[j];
+                if (token < 0 && at > target) {
+                    token = e + j;
+                    logit = x[j];
                 }
             }
-        } else if (lane == 0) {  // tokens too light to count one by one: the last of them
-            uint32_t last = 1;
-            for (int u = 0; u < units; ++u) last = max(last, S.last[u]);
-            token = (int)last - 1;
-            logit = load<DT>(row, token);
         }
         if (token >= 0) {
             P.tokens[r] = token;
