@@ -140,8 +140,8 @@ class DraftHead:
     """
 
     def __init__(self, w, bias=None, *, max_rows, logits_dtype="f32", device="cuda:0"):
-        self.device = torch.device(device)
-        w = (w if torch.is_tensor(w) else _dev(w, self.device)).to(self.device).contiguous()
+        w = (w if torch.is_tensor(w) else _dev(w, device)).to(device).contiguous()
+        self.device = w.device
         self.V, self.d = w.shape
         self.max_rows, self.logits_dtype = int(max_rows), logits_dtype
         if bias is not None:
@@ -161,8 +161,9 @@ class DraftHead:
             raise dcd.DcdError(dcd.DCD_ERR_SHAPE)
         self.workspace = torch.empty(self.ws_bytes, **u8)
         stream = torch.cuda.current_stream(self.device)
-        dcd.quantize_fp8(w, self.w, self.w_scale, rows=self.V, cols=self.d, dtype=self._name(w), block_rows=128,
-                         stream=stream)
+        with torch.cuda.device(self.device):
+            dcd.quantize_fp8(w, self.w, self.w_scale, rows=self.V, cols=self.d, dtype=self._name(w), block_rows=128,
+                             stream=stream)
         stream.synchronize()  # `w` may go; any stream may use the codes
 
     @staticmethod
@@ -200,13 +201,14 @@ class DraftHead:
                 (("probs", probs, (rows, self.V), f32), ("logprob", logprob, (rows,), f32), ("kept", kept, (rows,), i32))]
         if stream is None:
             stream = torch.cuda.current_stream(self.device)
-        dcd.quantize_fp8(h, self.h, self.h_scale, rows=rows, cols=self.d, dtype=self._name(h), stream=stream)
-        dcd.logits_fp8(dcd.make_fp8_problem(rows, self.V, self.d, self.logits_dtype),
-                       dcd.make_fp8_inputs(self.h, self.h_scale, self.w, self.w_scale, self.bias),
-                       self.logits, stream)
-        dcd.sample(dcd.make_sample_problem(rows, self.V, self.logits_dtype),
-                   dcd.make_sample_inputs(self.logits, u, *rules), dcd.make_sample_outputs(tokens, *outs),
-                   self.workspace, self.ws_bytes, stream)
+        with torch.cuda.device(self.device):  # (its default stream is NULL: the current device's)
+            dcd.quantize_fp8(h, self.h, self.h_scale, rows=rows, cols=self.d, dtype=self._name(h), stream=stream)
+            dcd.logits_fp8(dcd.make_fp8_problem(rows, self.V, self.d, self.logits_dtype),
+                           dcd.make_fp8_inputs(self.h, self.h_scale, self.w, self.w_scale, self.bias),
+                           self.logits, stream)
+            dcd.sample(dcd.make_sample_problem(rows, self.V, self.logits_dtype),
+                       dcd.make_sample_inputs(self.logits, u, *rules), dcd.make_sample_outputs(tokens, *outs),
+                       self.workspace, self.ws_bytes, stream)
 
     def propose(self, h, u, *, want_probs=True, **rules) -> dict:
         """One synchronous step on numpy (or torch) inputs; returns host copies of the outputs."""
