@@ -127,19 +127,9 @@ __device__ __forceinline__ void read_rows(u32x4 &a0, u32x4 &a1, float &s, uint32
                  : "memory");
 }
 
-constexpr int TILE = 16 * kGroup;  // bytes of 16 rows x 128 columns
+__device__ __forceinline__ uint32_t piece_offset() { return (uint32_t)piece_at(threadIdx.x % 64); }
 
-// Offset of a lane's first piece in such a tile in LDS.  A tile is 16 rows of 128 bytes; the
-// 16-byte column c of row r lies at c ^ (r % 8), so that the 16 rows of a matrix operand fall
-// into different banks.  (Its second piece, 64 columns on, lies at the address with bit 6
-// flipped: tiles start at multiples of 128.)
-__device__ __forceinline__ uint32_t piece_offset() {
-    const int lane = threadIdx.x % 64, n = lane % 16, g = lane / 16;
-    return (uint32_t)(n * kGroup + (g ^ n % 8) * 16);
-}
-
-// Half a tile (8 rows) from memory into LDS: lane l lands at byte 16 l, which holds column
-// (l % 8) ^ (l / 8) of row l / 8.
+// Half a tile (8 rows) from memory into LDS.
 template <int AUX>
 __device__ __forceinline__ void load_half(const uint8_t *base, uint32_t off, char *to) {
     __builtin_amdgcn_global_load_lds(base + off, (lds_ptr)to, 16, 0, AUX);

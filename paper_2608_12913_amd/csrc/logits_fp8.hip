@@ -70,18 +70,18 @@ __device__ __forceinline__ void stream_body(const Fp8Problem &P, char *lds) {
     auto block = [&](int i) { return b0 + (i + rot < nb ? i + rot : i + rot - nb); };
 
     const uint8_t *w = P.w + (size_t)base * P.K;
-    const uint32_t col = (lane % 8 ^ lane / 8) * 16;
+    const uint32_t col = half_column(lane);
     uint32_t woff[2 * TB], hoff[HT];
 #pragma unroll
-    for (int q = 0; q < 2 * TB; ++q) woff[q] = (uint32_t)min(8 * q + lane / 8, P.N - 1 - base) * (uint32_t)P.K;
+    for (int q = 0; q < 2 * TB; ++q) woff[q] = (uint32_t)min(8 * q + half_row(lane), P.N - 1 - base) * (uint32_t)P.K;
     const int half0 = KS == 1 ? wave * HT % (2 * RB) : 0;  // this wave's halves of the hidden-state tiles
 #pragma unroll
-    for (int q = 0; q < HT; ++q) hoff[q] = (uint32_t)min(8 * (half0 + q) + lane / 8, P.M - 1) * (uint32_t)P.K;
+    for (int q = 0; q < HT; ++q) hoff[q] = (uint32_t)min(8 * (half0 + q) + half_row(lane), P.M - 1) * (uint32_t)P.K;
     // the scales it loads: lanes 0-15 those of 16 rows, lane 16 its tokens' (KS = 4: all rows')
     const float *wscale = P.ws + (size_t)(base / kGroup) * P.groups;
     const float *rscale = P.hs + (size_t)min(KS == 1 ? wave % RB * 16 + n : lane, P.M - 1) * P.groups;
     const float *scale = KS == 1 && lane >= 16 ? wscale : rscale;
-    auto column = [&](int i) { return min((uint32_t)block(i) * kGroup + col, (uint32_t)P.K - 16); };
+    auto column = [&](int i) { return load_column(block(i), col, (uint32_t)P.K); };
     int fill = 0, hfill = 0;  // the slots to be filled next
     auto fetch = [&](int t, uint32_t k) {
 #pragma unroll

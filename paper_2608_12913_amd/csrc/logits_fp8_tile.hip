@@ -30,36 +30,6 @@
 namespace dcd {
 namespace {
 
-constexpr int TT = 256;                 // tokens per workgroup
-constexpr int VB = 4;                   // token blocks per wave
-constexpr int WT = 16 * VB;             // tokens per wave
-constexpr int WSTAGE = TT * kGroup;     // bytes of a weight stage
-constexpr int WL = WT / 8;              // a loading wave's instructions per weight stage
-constexpr int SB = 4;                   // blocks whose scales are loaded together
-
-template <int RB>
-struct TileGeo {
-    static constexpr int QB = RB / 2;          // row blocks per wave and hidden-state stage
-    static constexpr int TR = 32 * RB;         // rows per workgroup
-    static constexpr int HALF = 16 * QB;       // rows of a stage that one half of the waves multiplies
-    static constexpr int HL = QB;              // a loading wave's instructions per stage
-    static constexpr int HSTAGE = 2 * HALF * kGroup;
-    static constexpr int NW = 2, NH = 5;       // stages of the rings (more of either gain nothing)
-    // scales of SB blocks, two stages; each wave loads those of 64 rows, the last one past the tile's
-    static constexpr int SSTAGE = (TR + 64 - 8 * RB) * SB * 4;
-    static constexpr int SAT = NW * WSTAGE + NH * HSTAGE;
-    static constexpr int BAT = SAT + 2 * SSTAGE;   // bias of the tokens
-    static constexpr int LDS = BAT + TT * 4;
-    static_assert(RB == 4 || RB == 6, "operands of two or three row blocks");
-};
-
-// The token (of a wave's 64) at row r of its tiles in LDS.  Block v = 16 rows, and a lane's results
-// are rows 4 g .. 4 g + 3 of each: this way those of two blocks are 8 tokens in a row, and the four
-// lanes of a row of logits write 64 (bf16) or 128 bytes in a row.
-__device__ __forceinline__ constexpr int token_of(int r) {
-    return r / 32 * 32 + r % 16 / 4 * 8 + r / 16 % 2 * 4 + r % 4;
-}
-
 // Ends a slot: the wave's LDS reads have returned before it arrives, its loads stay in flight.
 __device__ __forceinline__ void slot_end() {
     asm volatile("" ::: "memory");
@@ -96,37 +66,32 @@ struct Loader {
 
     __device__ __forceinline__ void init(const Fp8Problem &P, int tok0, int row0, int wv, int start) {
         const int lane = threadIdx.x % 64;
-        col = (uint32_t)(lane % 8 ^ lane / 8) * 16;
+        col = (uint32_t)half_column(lane);
         K = (uint32_t)P.K;
         nb = P.groups;
         rot = start;
         if constexpr (G == 0) {
             const int t0 = tok0 + WT * wv;
             codes = Rows(P.w + (size_t)t0 * K, P.N - t0, K);
-            off = (uint32_t)token_of(lane / 8) * K;
+            off = (uint32_t)token_of(half_row(lane)) * K;
             lds_codes = wv * WT * kGroup;
         } else {
-            // waves 0, 1 load the rows of the first half of the waves, 2, 3 those of the second
             codes = Rows(P.h + (size_t)row0 * K, P.M - row0, K);
             scales = Rows(P.hs + (size_t)row0 * P.groups, P.M - row0, (uint32_t)P.groups * 4);
-            off = (uint32_t)(wv / 2 * 16 * RB + wv % 2 * 8 * Q::QB + lane / 8) * K;
+            off = (uint32_t)(first_row(RB, wv) + half_row(lane)) * K;
             lds_codes = wv * 8 * Q::QB * kGroup;
-            soff = (uint32_t)(wv * 8 * RB + lane) * (uint32_t)P.groups * 4;
-            lds_scale = wv * 8 * RB * SB * 4;
+            soff = (uint32_t)(wv * Q::SROWS + lane) * (uint32_t)P.groups * 4;
+            lds_scale = wv * Q::SROWS * SB * 4;
         }
     }
-    // The b-th block of the walk along K; past the last one: that one again (never read).
-    __device__ __forceinline__ int block(int b) const {
-        b = min(b, nb - 1) + rot;
-        return b < nb ? b : b - nb;
-    }
+    __device__ __forceinline__ int block(int b) const { return walk_block(b, nb, rot); }
     // Block b's stage (hidden states: part `par` of the rows) into `to`.
     struct Request {
         uint32_t at;
         char *to;
     };
     __device__ __forceinline__ Request request(int b, int par, char *to) const {
-        Request r{off + min((uint32_t)block(b) * kGroup + col, K - 16) + (G == 0 ? 0u : (uint32_t)(par * Q::HALF) * K),
+        Request r{off + load_column(block(b), col, K) + (G == 0 ? 0u : (uint32_t)(par * Q::HALF) * K),
                   to + lds_codes};
         asm volatile("" : "+v"(r.at));  // made here, not between the products that the loads are spread over
         return r;
@@ -259,7 +224,7 @@ template <int RB, int G, int DT>
 __device__ __forceinline__ void work(const Fp8Problem &P, char *lds, int tok0, int row0, int wv, int start) {
     using Q = TileGeo<RB>;
     constexpr int QB = Q::QB, NW = Q::NW, NH = Q::NH;
-    static_assert(NH - 2 < 2 * SB - 1, "scales have landed before they are read");
+    static_assert(Q::HAHEAD < 2 * SB - 1, "scales have landed before they are read");
     const int lane = threadIdx.x % 64, n = lane % 16, g = lane / 16;
     char *hring = lds + NW * WSTAGE, *sring = lds + Q::SAT;
     Loader<RB, G> ld;
@@ -310,7 +275,7 @@ __device__ __forceinline__ void work(const Fp8Problem &P, char *lds, int tok0, i
 #pragma unroll
                 for (int v = 0; v < VB; ++v) wa[v].set(o.a[2 * v], o.a[2 * v + 1]);
             }
-            if constexpr (G == 1) wait_loads<(NH - 2) * Q::HL>();
+            if constexpr (G == 1) wait_loads<Q::HAHEAD * Q::HL>();
             // G = 1: stage 2 c + par + NH
             const auto req = G == 0 ? ld.request(c + NW, 0, lds + wcur)
                                     : ld.request(c + (par + NH) / 2, (par + NH) % 2, hring + hcur);
@@ -327,7 +292,7 @@ __device__ __forceinline__ void work(const Fp8Problem &P, char *lds, int tok0, i
             else
                 multiply<RB, QB, QB - 1>(o, wa, wsc, pend, acc, ld, req, LO, HI);
             if constexpr (G == 0) {
-                if (par == 1) wait_loads<(NW - 1) * WL>();
+                if (par == 1) wait_loads<Q::WAHEAD * WL>();
             }
             slot_end();
             hcur = next(hcur, Q::HSTAGE, NH * Q::HSTAGE);
@@ -398,13 +363,10 @@ __device__ __forceinline__ void tile_body(const Fp8Problem &P, int nrow, char *l
     const int xcd = blockIdx.x % kXcds, at = blockIdx.x / kXcds;
     const int tok0 = (at / nrow * kXcds + xcd) * TT, row0 = at % nrow * TileGeo<RB>::TR;
     if (tok0 >= P.N) return;
-    // Where every weight is read once (one tile of rows), the walk along K starts at another block for
-    // each tile of tokens, so that the chip does not ask all HBM channels for the same columns at once
-    // (scales are loaded SB blocks at a time, so only where their number divides).  From the first
-    // block and like this, us, 100 rows in bf16, d = 2048, 4096, 6144, 8192, 16384: 65,536 tokens 42 and 42, 76 and
-    // 71, 105 and 102, 142 and 133, 256 and 252; 128,256 tokens, 4096: 150 and 140.  With more rows the weights come
-    // from the caches: 512 rows of 65,536, 8192 467 and 487, 1024 of 6144 685 and 721.
-    const int start = nrow == 1 && P.groups % SB == 0 ? (int)((unsigned)(tok0 / TT) * SB % (unsigned)P.groups) : 0;
+    // From the first block and from a block of its own, us, 100 rows in bf16, d = 2048, 4096, 6144, 8192, 16384:
+    // 65,536 tokens 42 and 42, 76 and 71, 105 and 102, 142 and 133, 256 and 252; 128,256 tokens, 4096: 150 and 140.
+    // With more rows the weights come from the caches: 512 rows of 65,536, 8192 467 and 487, 1024 of 6144 685 and 721.
+    const int start = walk_start(tok0 / TT, nrow, P.groups);
     if (wave < 4)
         work<RB, 0, DT>(P, lds, tok0, row0, wave, start);
     else

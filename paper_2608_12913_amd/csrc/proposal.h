@@ -5,11 +5,10 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "logits_fp8_geo.h"
 #include "route.h"
 
 namespace dcd {
-
-constexpr int kGroup = 128;  // elements of K that share a scale
 
 struct QuantProblem {
     long long rows;
