@@ -88,3 +88,14 @@ def test_repeats_and_replays(M):
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, _run(t, M, N, K, "bf16"))
+
+
+@pytest.mark.parametrize("M, more", [(5, 16), (20, 60), (70, 128), (300, 520)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_do_not_depend_on_the_rows_beside_them(M, more, dtype):
+    """A batch's first rows alone: the same bits, where both batches add the blocks of K in one order (up to
+    64 rows; one tile of 128 rows, which every number of rows up to that takes; several tiles)."""
+    N, K = 13000, 1024
+    h, hs, w, ws, bias = _dev(*_inputs(more, N, K, M))
+    some = [h[:M].contiguous(), hs[:M].contiguous(), w, ws, bias]
+    assert torch.equal(_run(some, M, N, K, dtype), _run([h, hs, w, ws, bias], more, N, K, dtype)[:M])
