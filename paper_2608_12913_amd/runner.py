@@ -186,8 +186,10 @@ class DraftHead:
                min_p=None, logprob=None, kept=None, stream=None) -> None:
         """Enqueue one step on `stream` (default: torch's current stream): h [rows, d] bf16 or fp32,
         u [rows] and the rules (each None or [rows]); tokens int32 and, where given, probs [rows, V], logprob and
-        kept are written.  tokens and probs may be a :class:`DeviceProblem`'s tokens and
-        draft_probs, where row b * N + i proposes node i of sequence b."""
+        kept are written, each dense.  tokens and probs may be a :class:`DeviceProblem`'s tokens and
+        draft_probs [B * N, V], where row b * N + i proposes node i of sequence b: one step then draws all
+        of their rows (node i of every sequence alone lies N rows apart: draw into buffers of the
+        step's own and copy)."""
         rows = int(h.shape[0])
         if rows > self.max_rows:
             raise ValueError(f"{rows} rows, room for {self.max_rows}")
